@@ -317,13 +317,12 @@ def _run_own(s):
         y = mixer.scan_step(s["x"], s["dt"], s["A"], s["B"], s["C"], s["s0"], s["D"], s["bias"], softplus=True,
                             state_out=state)
         return dict(y=y, state=state)
-    train = case["way"] == "train"
-    y, state, saved = mixer.scan_fwd(s["x"], s["dt"], s["A"], s["B"], s["C"], s["D"], s["bias"], s["s0"],
-                                     cu_seqlens=s["cu"], softplus=True, save_states=train)
+    y, state = mixer.scan_fwd(s["x"], s["dt"], s["A"], s["B"], s["C"], s["D"], s["bias"], s["s0"], cu_seqlens=s["cu"],
+                              softplus=True)
     res = dict(y=y, state=state)
-    if train:
-        d = mixer.scan_bwd(s["x"], s["dt"], s["A"], s["B"], s["C"], s["D"], s["bias"], s["s0"], saved, s["dy"],
-                           s["dsf"], cu_seqlens=s["cu"], softplus=True, need_d_initial_state=case["state"])
+    if case["way"] == "train":
+        d = mixer.scan_bwd(s["x"], s["dt"], s["A"], s["B"], s["C"], s["D"], s["bias"], s["s0"], s["dy"], s["dsf"],
+                           cu_seqlens=s["cu"], softplus=True, need_d_initial_state=case["state"])
         res.update(dx=d["dx"], ddt=d["ddt"], dA=d["dA"], dB=d["dB"], dC=d["dC"], dD=d["dD"], dbias=d["ddt_bias"],
                    ds0=d["d_initial_state"])
     return {k: v for k, v in res.items() if v is not None}

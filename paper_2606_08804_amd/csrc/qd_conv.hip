@@ -1,0 +1,326 @@
+// Short causal depthwise convolution along the tokens of each sequence, with
+// bias and SiLU: prompts (dense or packed), their backward, and single tokens.
+//
+//   u_t = b + sum_j w[:, j] x_{t - W + 1 + j},   y = u  or  u sigmoid(u)
+//   backward, du = dy (SiLU'(u)):  dx_t = sum_j w[:, j] du_{t + W - 1 - j},
+//             dw[:, j] = sum_t du_t x_{t - W + 1 + j},  db = sum_t du_t
+//
+// x before a sequence's first token are the rows of its state [W - 1][D], the
+// oldest first, or zero.  A thread owns V channels (16 bytes) and walks a tile
+// of tokens with the last W - 1 rows in registers, so a row is read once and the
+// W - 1 rows before a tile (after it, in the backward, which forms u again)
+// twice.  HBM bounds all of it.  The weight's gradient is summed in registers
+// over a wave's tile, over the workgroup's four tiles in LDS and over the
+// workgroups by a second launch, each in a fixed order.
+#include "qd_mixer.h"
+
+namespace qd {
+
+namespace {
+
+constexpr int BT = 32;             // backward: tokens of a wave's tile
+constexpr int BSLOT = 4 * BT;      // ... and of a workgroup's
+
+// Row `pos` of a sequence (negative: the state's, or zero without one).
+template <typename E, int V, int W>
+__device__ inline void load_row(Vec<E, V>& r, const ConvArgs& a, int n, long s, int pos, int c) {
+  if (pos >= 0) r.load((const E*)a.x + (s + pos) * a.ldx + c);
+  else if (a.s0) r.load((const E*)a.s0 + ((long)n * (W - 1) + W - 1 + pos) * a.D + c);
+  else r.zero();
+}
+
+template <typename E, int V, int W>
+__device__ inline void load_weights(float (&w)[W][V], float (&b)[V], const ConvArgs& a, int c) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    b[i] = a.b ? tof(((const E*)a.b)[c + i]) : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j][i] = tof(((const E*)a.w)[(long)(c + i) * W + j]);
+  }
+}
+
+// Tiles of L tokens by flat thread index, then the final states by further threads.
+template <typename E, int V, int W>
+__global__ __launch_bounds__(NTHREADS) void k_conv_fwd(ConvArgs a, int L, long tile_threads) {
+  constexpr int U = 8;             // tokens whose loads are in flight together
+  const int nv = a.D / V;
+  long i = (long)blockIdx.x * NTHREADS + threadIdx.x;
+  int n, len, pos;
+  long s;
+  if (i >= tile_threads) {         // one piece of a final state row
+    i -= tile_threads;
+    if (!a.sf || i >= (long)a.q.N * (W - 1) * nv) return;
+    const int c = (int)(i % nv) * V, j = (int)(i / nv % (W - 1));
+    n = (int)(i / nv / (W - 1));
+    if (!a.q.range(n, s, len)) return;
+    Vec<E, V> r;
+    load_row<E, V, W>(r, a, n, s, len - (W - 1) + j, c);
+    r.store((E*)a.sf + ((long)n * (W - 1) + j) * a.D + c);
+    return;
+  }
+  const long slot = i / nv;
+  const int c = (int)(i - slot * nv) * V;
+  if (slot >= a.q.slots(L) || !a.q.locate(slot, L, n, s, len, pos)) return;
+  const int end = min(pos + L, len);
+  float w[W][V], b[V];
+  load_weights<E, V, W>(w, b, a, c);
+  Vec<E, V> x[W - 1 + U];
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) load_row<E, V, W>(x[j], a, n, s, pos - (W - 1) + j, c);
+  E* y = (E*)a.y + s * a.D + c;
+  const E* xp = (const E*)a.x + s * a.ldx + c;
+  for (; pos < end; pos += U) {
+#pragma unroll
+    for (int k = 0; k < U; ++k)
+      if (pos + k < end) x[W - 1 + k].load(xp + (long)(pos + k) * a.ldx);
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      if (pos + k >= end) break;
+      Vec<E, V> o;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float u = b[e];
+#pragma unroll
+        for (int j = 0; j < W; ++j) u += w[j][e] * x[k + j].v[e];
+        o.v[e] = a.silu ? u * fast_sigmoid(u) : u;
+      }
+      o.store(y + (long)(pos + k) * a.D);
+    }
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) x[j] = x[U + j];
+  }
+}
+
+// du from u and dy.
+__device__ inline float act_grad(float u, float dy, int silu) {
+  if (!silu) return dy;
+  const float sg = fast_sigmoid(u);
+  return dy * (sg * (1.f + u * (1.f - sg)));
+}
+
+// Workgroup: 64 pieces of channels (one a lane) by four successive tiles of BT
+// tokens (one a wave); grid: slots of BSLOT tokens by groups of 64 pieces.
+template <typename E, int V, int W>
+__global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups) {
+  constexpr int U = 4, R = W + 1;
+  __shared__ float sum[R][64 * V];
+  const long slot = blockIdx.x / cgroups;
+  const int cg = (int)(blockIdx.x - slot * cgroups), lane = threadIdx.x & 63, wave = wave_id(threadIdx.x);
+  const int c = (cg * 64 + lane) * V;
+  const bool mine = c < a.D;
+  float dw[R][V] = {};             // W taps, then the bias
+  int n, len, pos;
+  long s;
+  if (a.q.locate(slot, BSLOT, n, s, len, pos) && mine && pos + wave * BT < len) {
+    pos += wave * BT;
+    const int end = min(pos + BT, len), stop = min(end + W - 1, len);
+    float w[W][V], b[V];
+    load_weights<E, V, W>(w, b, a, c);
+    Vec<E, V> x[W - 1 + U];
+    float du[W - 1 + U][V];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) {
+      load_row<E, V, W>(x[j], a, n, s, pos - (W - 1) + j, c);
+#pragma unroll
+      for (int e = 0; e < V; ++e) du[j][e] = 0.f;       // read for rows before the tile only, which are not written
+    }
+    const E* xp = (const E*)a.x + s * a.ldx + c;
+    const E* gp = (const E*)a.dy + s * a.D + c;
+    E* dx = (E*)a.dx + s * a.D + c;
+    for (int t0 = pos; t0 < end + W - 1; t0 += U) {
+      Vec<E, V> g[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        g[k].zero();
+        if (t0 + k < stop) {
+          x[W - 1 + k].load(xp + (long)(t0 + k) * a.ldx);
+          g[k].load(gp + (long)(t0 + k) * a.D);
+        } else {
+          x[W - 1 + k].zero();
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int t = t0 + k;                            // du_t, then the row t - (W - 1) of dx
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          float u = b[e];
+#pragma unroll
+          for (int j = 0; j < W; ++j) u += w[j][e] * x[k + j].v[e];
+          const float d = t < stop ? act_grad(u, g[k].v[e], a.silu) : 0.f;
+          du[W - 1 + k][e] = d;
+          if (t < end) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) dw[j][e] += d * x[k + j].v[e];
+            dw[W][e] += d;
+          }
+        }
+        const int p = t - (W - 1);
+        if (p < pos || p >= end) continue;
+        Vec<E, V> o;
+        if (a.dsf && p >= len - (W - 1)) o.load((const E*)a.dsf + ((long)n * (W - 1) + p - (len - (W - 1))) * a.D + c);
+        else o.zero();
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+#pragma unroll
+          for (int j = 0; j < W; ++j) o.v[e] += w[j][e] * du[W - 1 + k - j][e];
+        o.store(dx + (long)p * a.D);
+      }
+#pragma unroll
+      for (int j = 0; j < W - 1; ++j) {
+        x[j] = x[U + j];
+#pragma unroll
+        for (int e = 0; e < V; ++e) du[j][e] = du[U + j][e];
+      }
+    }
+  }
+  for (int turn = 0; turn < 4; ++turn) {
+    if (wave == turn)
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum[r][lane * V + e] = (turn ? sum[r][lane * V + e] : 0.f) + dw[r][e];
+    __syncthreads();
+  }
+  for (int k = threadIdx.x; k < R * 64 * V; k += NTHREADS) {
+    const int r = k / (64 * V), d = cg * 64 * V + k % (64 * V);
+    if (d < a.D) a.part[(slot * R + r) * a.D + d] = sum[r][k % (64 * V)];
+  }
+}
+
+// Gradient of the initial state: row i of it is x at position i - (W - 1).
+template <typename E, int V, int W>
+__global__ __launch_bounds__(NTHREADS) void k_conv_ds0(ConvArgs a) {
+  const int nv = a.D / V;
+  const long k = (long)blockIdx.x * NTHREADS + threadIdx.x;
+  if (k >= (long)a.q.N * (W - 1) * nv) return;
+  const int c = (int)(k % nv) * V, i = (int)(k / nv % (W - 1)), n = (int)(k / nv / (W - 1));
+  int len;
+  long s;
+  if (!a.q.range(n, s, len)) return;
+  float w[W][V], b[V];
+  load_weights<E, V, W>(w, b, a, c);
+  Vec<E, V> o;
+  if (a.dsf && i >= len) o.load((const E*)a.dsf + ((long)n * (W - 1) + i - len) * a.D + c);   // that row is still in the final state
+  else o.zero();
+  // token t reads the row with tap i - t
+  Vec<E, V> x[2 * W - 2];
+#pragma unroll
+  for (int j = 0; j < 2 * W - 2; ++j) {
+    if (j < W - 1 + min(len, W - 1)) load_row<E, V, W>(x[j], a, n, s, j - (W - 1), c);
+    else x[j].zero();
+  }
+#pragma unroll
+  for (int t = 0; t < W - 1; ++t) {
+    if (t >= len || t > i) continue;
+    Vec<E, V> g;
+    g.load((const E*)a.dy + (s + t) * a.D + c);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float u = b[e], tap = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        u += w[j][e] * x[t + j].v[e];
+        if (j == i - t) tap = w[j][e];
+      }
+      o.v[e] += tap * act_grad(u, g.v[e], a.silu);
+    }
+  }
+  o.store((E*)a.ds0 + ((long)n * (W - 1) + i) * a.D + c);
+}
+
+// One token: a thread owns V channels of one sequence and reads all of its rows before it writes.
+template <typename E, int V, int W>
+__global__ __launch_bounds__(64) void k_conv_step(ConvArgs a) {
+  const int nv = a.D / V;
+  const long k = (long)blockIdx.x * 64 + threadIdx.x;
+  if (k >= (long)a.q.N * nv) return;
+  const int n = (int)(k / nv), c = (int)(k - (long)n * nv) * V;
+  Vec<E, V> x[W], o;
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) x[j].load((const E*)a.s0 + ((long)n * (W - 1) + j) * a.D + c);
+  x[W - 1].load((const E*)a.x + n * a.ldx + c);
+  float w[W][V], b[V];
+  load_weights<E, V, W>(w, b, a, c);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    float u = b[e];
+#pragma unroll
+    for (int j = 0; j < W; ++j) u += w[j][e] * x[j].v[e];
+    o.v[e] = a.silu ? u * fast_sigmoid(u) : u;
+  }
+  o.store((E*)a.y + (long)n * a.D + c);
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) x[j + 1].store((E*)a.sf + ((long)n * (W - 1) + j) * a.D + c);
+}
+
+template <typename E, int V, int W>
+hipError_t fwd(const ConvArgs& a, hipStream_t st) {
+  const int nv = a.D / V;
+  const long tokens = a.q.cu ? a.q.T : (long)a.q.N * a.q.T;
+  // Tiles of 32 tokens once they give every CU eight waves, else of 8: short
+  // prompts need the threads more than they save rows read twice.
+  const int L = tokens / 32 * nv >= 1 << 17 ? 32 : 8;
+  const long tiles = a.q.slots(L) * nv, states = a.sf ? (long)a.q.N * (W - 1) * nv : 0;
+  if (tiles + states == 0) return hipSuccess;
+  const dim3 grid((unsigned)((tiles + states + NTHREADS - 1) / NTHREADS));
+  hipLaunchKernelGGL((k_conv_fwd<E, V, W>), grid, dim3(NTHREADS), 0, st, a, L, tiles);
+  return hipGetLastError();
+}
+
+template <typename E, int V, int W>
+hipError_t bwd(const ConvArgs& a, hipStream_t st) {
+  const int cgroups = (a.D / V + 63) / 64;
+  const long slots = conv_bwd_slots(a.q);
+  if (slots > 0) hipLaunchKernelGGL((k_conv_bwd<E, V, W>), dim3((unsigned)(slots * cgroups)), dim3(NTHREADS), 0, st, a, cgroups);
+  const long states = a.ds0 ? (long)a.q.N * (W - 1) * (a.D / V) : 0;
+  if (states > 0)
+    hipLaunchKernelGGL((k_conv_ds0<E, V, W>), dim3((unsigned)((states + NTHREADS - 1) / NTHREADS)), dim3(NTHREADS), 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename E, int V, int W>
+hipError_t step(const ConvArgs& a, hipStream_t st) {
+  const long n = (long)a.q.N * (a.D / V);
+  if (n > 0) hipLaunchKernelGGL((k_conv_step<E, V, W>), dim3((unsigned)((n + 63) / 64)), dim3(64), 0, st, a);
+  return hipGetLastError();
+}
+
+bool whole(const ConvArgs& a, int esz) {
+  const int v = 16 / esz;
+  uintptr_t p = 0;
+  for (const void* q : {a.x, a.s0, (const void*)a.y, (const void*)a.sf, a.dy, a.dsf, (const void*)a.dx, (const void*)a.ds0})
+    p |= (uintptr_t)q;
+  return a.D % v == 0 && a.ldx % v == 0 && (p & 15) == 0;
+}
+
+#define QD_CONV(FN)                                                                                                    \
+  template <typename E, int V>                                                                                         \
+  hipError_t FN##_w(const ConvArgs& a, hipStream_t st) {                                                               \
+    return a.W == 2 ? FN<E, V, 2>(a, st) : a.W == 3 ? FN<E, V, 3>(a, st) : a.W == 4 ? FN<E, V, 4>(a, st)               \
+                                                                                    : hipErrorInvalidValue;            \
+  }                                                                                                                    \
+  hipError_t FN##_e(const ConvArgs& a, int dtype, hipStream_t st) {                                                    \
+    if (dtype == 1) return whole(a, 2) ? FN##_w<__bf16, 8>(a, st) : FN##_w<__bf16, 1>(a, st);                          \
+    return whole(a, 4) ? FN##_w<float, 4>(a, st) : FN##_w<float, 1>(a, st);                                            \
+  }
+QD_CONV(fwd)
+QD_CONV(bwd)
+QD_CONV(step)
+#undef QD_CONV
+
+}  // namespace
+
+long conv_bwd_slots(const Seqs& q) { return q.slots(BSLOT); }
+
+hipError_t launch_conv_fwd(const ConvArgs& a, int dtype, hipStream_t st) { return fwd_e(a, dtype, st); }
+
+hipError_t launch_conv_bwd(const ConvArgs& a, int dtype, hipStream_t st) {
+  const hipError_t e = bwd_e(a, dtype, st);
+  if (e != hipSuccess || (!a.dw && !a.db)) return e;
+  return launch_colsum(a.part, (int)conv_bwd_slots(a.q), a.W + 1, a.W, a.D, dtype, a.dw, a.db, st);
+}
+
+hipError_t launch_conv_step(const ConvArgs& a, int dtype, hipStream_t st) { return step_e(a, dtype, st); }
+
+}  // namespace qd

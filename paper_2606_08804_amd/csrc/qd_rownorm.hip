@@ -1,0 +1,312 @@
+// Row normalisation with weight, bias and a SiLU gate, forward and backward,
+// and the sum of partial columns that this file's and the convolution's weight
+// gradients end with.
+//
+//   xh = (x - mean) r,  r = 1 / sqrt(var + eps)      ("rms": mean = 0, var = mean of x^2)
+//   y  = (xh w + b) s,  s = g sigmoid(g)             (s = 1 without a gate)
+//   backward, d = dy s w:  dx = r (d - mean(d) - xh mean(d xh))  ("rms": without mean(d))
+//             dw = sum dy s xh,  db = sum dy s,  dg = dy (xh w + b) sigmoid(g) (1 + g (1 - sigmoid(g)))
+//
+// Both directions are bound by HBM: a row is read once into registers (LANES
+// lanes with K pieces of V elements each) and everything that needs its sums is
+// formed from there.  The backward's row groups walk rows with the weight's
+// gradient in registers, sum it over the workgroup in LDS and write one partial
+// row per workgroup; no atomics, so results do not change from run to run.
+#include "qd_mixer.h"
+
+namespace qd {
+
+namespace {
+
+// Sum over the LANES lanes of a row, the same value in each of them.
+template <int LANES>
+__device__ inline float row_sum(float x, float* red) {
+  x = sum16(x);
+  if constexpr (LANES >= 64) {
+    x += __shfl_xor(x, 16, 64);
+    x += __shfl_xor(x, 32, 64);
+  }
+  if constexpr (LANES == 256) {
+    const int w = threadIdx.x >> 6;
+    __syncthreads();                       // the last sum has been read
+    if ((threadIdx.x & 63) == 0) red[w] = x;
+    __syncthreads();
+    x = (red[0] + red[1]) + (red[2] + red[3]);
+  }
+  return x;
+}
+
+template <typename E, int V, int LANES, int K>
+__global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
+  __shared__ float red[4];
+  constexpr int RPB = NTHREADS / LANES;
+  const long row = (long)blockIdx.x * RPB + threadIdx.x / LANES;
+  const int lane = threadIdx.x % LANES;
+  if (row >= a.rows) return;               // LANES == 256: never; else whole lane groups leave together
+  const E* x = (const E*)a.x + row * a.ldx;
+  Vec<E, V> v[K];
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * LANES + lane) * V;
+    if (c < a.D) v[k].load(x + c); else v[k].zero();
+#pragma unroll
+    for (int i = 0; i < V; ++i) s += v[k].v[i];
+  }
+  const float inv = 1.f / (float)a.D;
+  const float mean = a.rms ? 0.f : row_sum<LANES>(s, red) * inv;
+  float ss = 0.f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool in = (k * LANES + lane) * V < a.D;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[k].v[i] -= mean;
+      ss += in ? v[k].v[i] * v[k].v[i] : 0.f;
+    }
+  }
+  const float r = 1.f / sqrtf(row_sum<LANES>(ss, red) * inv + a.eps);
+  E* y = (E*)a.y + row * a.D;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c = (k * LANES + lane) * V;
+    if (c >= a.D) break;
+    Vec<E, V> w, b, g;
+    if (a.w) w.load((const E*)a.w + c);
+    if (a.b) b.load((const E*)a.b + c);
+    if (a.g) g.load((const E*)a.g + row * a.ldg + c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      float o = v[k].v[i] * r;
+      if (a.w) o *= w.v[i];
+      if (a.b) o += b.v[i];
+      if (a.g) o *= g.v[i] * fast_sigmoid(g.v[i]);
+      v[k].v[i] = o;
+    }
+    v[k].store(y + c);
+  }
+  if (a.stats && lane == 0) {
+    a.stats[2 * row] = mean;
+    a.stats[2 * row + 1] = r;
+  }
+}
+
+template <typename E, int V, int LANES, int K, bool GATE>
+__global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
+  __shared__ float red[4];
+  extern __shared__ float cols[];          // [2][LANES * K * V] where the workgroup has more than one row
+  constexpr int RPB = NTHREADS / LANES;
+  const int lane = threadIdx.x % LANES;
+  const float inv = 1.f / (float)a.D;
+  float dw[K * V] = {}, db[K * V] = {};
+  // LANES == 256: row is uniform over the workgroup, so its barriers are met by all
+  for (long row = (long)blockIdx.x * RPB + threadIdx.x / LANES; row < a.rows; row += (long)gridDim.x * RPB) {
+    Vec<E, V> xh[K], d[K], g[GATE ? K : 1];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * LANES + lane) * V;
+      xh[k].zero();
+      d[k].zero();
+      if (c < a.D) {
+        xh[k].load((const E*)a.x + row * a.ldx + c);
+        d[k].load((const E*)a.dy + row * a.D + c);
+        if constexpr (GATE) g[k].load((const E*)a.g + row * a.ldg + c);
+      } else if constexpr (GATE) {
+        g[k].zero();
+      }
+    }
+    const float mean = a.stats[2 * row], r = a.stats[2 * row + 1];
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * LANES + lane) * V;
+      const bool in = c < a.D;
+      Vec<E, V> w, b, o;
+      if (in && a.w) w.load((const E*)a.w + c);
+      if (GATE && in && a.b) b.load((const E*)a.b + c);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const float h = (xh[k].v[i] - mean) * r;
+        float e = d[k].v[i];
+        if constexpr (GATE) {
+          const float gv = g[k].v[i], sg = fast_sigmoid(gv);
+          float lin = h;
+          if (a.w) lin *= w.v[i];
+          if (a.b) lin += b.v[i];
+          o.v[i] = e * lin * (sg * (1.f + gv * (1.f - sg)));
+          e *= gv * sg;
+        }
+        if (in) {
+          dw[k * V + i] += e * h;
+          db[k * V + i] += e;
+        }
+        if (a.w) e *= w.v[i];
+        xh[k].v[i] = h;
+        d[k].v[i] = e;
+        if (in) {
+          s1 += e;
+          s2 += e * h;
+        }
+      }
+      if constexpr (GATE)
+        if (in) o.store((E*)a.dg + row * a.D + c);
+    }
+    s1 = a.rms ? 0.f : row_sum<LANES>(s1, red) * inv;
+    s2 = row_sum<LANES>(s2, red) * inv;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int c = (k * LANES + lane) * V;
+      if (c >= a.D) break;
+#pragma unroll
+      for (int i = 0; i < V; ++i) d[k].v[i] = r * (d[k].v[i] - s1 - xh[k].v[i] * s2);
+      d[k].store((E*)a.dx + row * a.D + c);
+    }
+  }
+  if (!a.part) return;
+  // one partial row [2][D] per workgroup: over the rows of a wave by lane moves, over the waves in order
+  if constexpr (LANES == 16) {
+#pragma unroll
+    for (int i = 0; i < K * V; ++i) {
+      dw[i] += __shfl_xor(dw[i], 16, 64);
+      dw[i] += __shfl_xor(dw[i], 32, 64);
+      db[i] += __shfl_xor(db[i], 16, 64);
+      db[i] += __shfl_xor(db[i], 32, 64);
+    }
+  }
+  float* out = a.part + (long)blockIdx.x * 2 * a.D;
+  if constexpr (LANES < 256) {
+    constexpr int N = LANES * K * V;
+    const int w = threadIdx.x >> 6;
+    for (int turn = 0; turn < 4; ++turn) {
+      if (w == turn && (threadIdx.x & 63) < LANES) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            const int c = (k * LANES + lane) * V + i;
+            cols[c] = (turn ? cols[c] : 0.f) + dw[k * V + i];
+            cols[N + c] = (turn ? cols[N + c] : 0.f) + db[k * V + i];
+          }
+      }
+      __syncthreads();
+    }
+    for (int c = threadIdx.x; c < a.D; c += NTHREADS) {
+      out[c] = cols[c];
+      out[a.D + c] = cols[N + c];
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = (k * LANES + lane) * V + i;
+        if (c < a.D) {
+          out[c] = dw[k * V + i];
+          out[a.D + c] = db[k * V + i];
+        }
+      }
+  }
+}
+
+// 64 columns by 16 row groups a workgroup.
+constexpr int CS_COLS = 64, CS_ROWS = 16;
+template <typename E>
+__global__ __launch_bounds__(CS_COLS* CS_ROWS) void k_colsum(const float* __restrict__ part, int n, int rows, int J,
+                                                             int D, E* __restrict__ w, E* __restrict__ b) {
+  __shared__ float red[CS_ROWS][CS_COLS];
+  const int c = threadIdx.x % CS_COLS, g = threadIdx.x / CS_COLS;
+  const long col = (long)blockIdx.x * CS_COLS + c;      // j * D + d
+  const long cols = (long)rows * D;
+  const int j = (int)(col / D);
+  const bool want = col < cols && (j < J ? w != nullptr : b != nullptr);
+  float s = 0.f;
+  if (want)
+#pragma unroll 8
+    for (int i = g; i < n; i += CS_ROWS) s += part[(long)i * cols + col];
+  red[g][c] = s;
+  __syncthreads();
+  if (g || !want) return;
+  for (int i = 1; i < CS_ROWS; ++i) s += red[i][c];
+  const int d = (int)(col - (long)j * D);
+  if (j < J) w[(long)d * J + j] = fromf<E>(s);
+  else b[d] = fromf<E>(s);
+}
+
+template <typename E, int V, int LANES, int K>
+hipError_t fwd(const RowNormArgs& a, hipStream_t st) {
+  constexpr int RPB = NTHREADS / LANES;
+  hipLaunchKernelGGL((k_norm_fwd<E, V, LANES, K>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(NTHREADS), 0, st, a);
+  return hipGetLastError();
+}
+
+template <typename E, int V, int LANES, int K>
+hipError_t bwd(const RowNormArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)norm_bwd_blocks(a.rows, a.D));
+  const size_t lds = LANES < 256 ? 2 * sizeof(float) * LANES * K * V : 0;
+  if (a.g) hipLaunchKernelGGL((k_norm_bwd<E, V, LANES, K, true>), grid, dim3(NTHREADS), lds, st, a);
+  else hipLaunchKernelGGL((k_norm_bwd<E, V, LANES, K, false>), grid, dim3(NTHREADS), lds, st, a);
+  return hipGetLastError();
+}
+
+// Lanes a row by its pieces: 16 lanes of one, a wave of one or four, else the workgroup.
+#define QD_ROWNORM(FN)                                             \
+  const int nv = (a.D + V - 1) / V;                                \
+  if (nv <= 16) return FN<E, V, 16, 1>(a, st);                     \
+  if (nv <= 64) return FN<E, V, 64, 1>(a, st);                     \
+  if (nv <= 256) return FN<E, V, 64, 4>(a, st);                    \
+  if (nv <= 1024) return FN<E, V, 256, 4>(a, st);                  \
+  if constexpr (V == 4)                                            \
+    if (nv <= 2048) return FN<E, V, 256, 8>(a, st);                \
+  if constexpr (V == 1)                                            \
+    if (nv <= 8192) return FN<E, V, 256, 32>(a, st);               \
+  return hipErrorInvalidValue
+
+template <typename E, int V>
+hipError_t by_size_fwd(const RowNormArgs& a, hipStream_t st) { QD_ROWNORM(fwd); }
+template <typename E, int V>
+hipError_t by_size_bwd(const RowNormArgs& a, hipStream_t st) { QD_ROWNORM(bwd); }
+#undef QD_ROWNORM
+
+// Whether every row of every tensor of the call is whole aligned 16-byte pieces.
+bool whole(const RowNormArgs& a, int esz) {
+  const int v = 16 / esz;
+  uintptr_t p = 0;
+  for (const void* q : {a.x, a.w, a.b, a.g, (const void*)a.y, a.dy, (const void*)a.dx, (const void*)a.dg})
+    p |= (uintptr_t)q;
+  return a.D % v == 0 && a.ldx % v == 0 && (!a.g || a.ldg % v == 0) && (p & 15) == 0;
+}
+
+}  // namespace
+
+// Workgroups of the backward: enough to fill the chip, few enough that their
+// partial rows (2 D floats each) stay small beside the tensors.
+int norm_bwd_blocks(long rows, int D) {
+  long n = (1L << 20) / D;
+  n = n < 256 ? 256 : n > 2048 ? 2048 : n;
+  return (int)(rows < n ? (rows < 1 ? 1 : rows) : n);
+}
+
+hipError_t launch_norm_fwd(const RowNormArgs& a, int dtype, hipStream_t st) {
+  if (dtype == 1) return whole(a, 2) ? by_size_fwd<__bf16, 8>(a, st) : by_size_fwd<__bf16, 1>(a, st);
+  return whole(a, 4) ? by_size_fwd<float, 4>(a, st) : by_size_fwd<float, 1>(a, st);
+}
+
+hipError_t launch_norm_bwd(const RowNormArgs& a, int dtype, hipStream_t st) {
+  hipError_t e;
+  if (dtype == 1) e = whole(a, 2) ? by_size_bwd<__bf16, 8>(a, st) : by_size_bwd<__bf16, 1>(a, st);
+  else e = whole(a, 4) ? by_size_bwd<float, 4>(a, st) : by_size_bwd<float, 1>(a, st);
+  if (e != hipSuccess || !a.part) return e;
+  return launch_colsum(a.part, norm_bwd_blocks(a.rows, a.D), 2, 1, a.D, dtype, a.dw, a.db, st);
+}
+
+hipError_t launch_colsum(const float* part, int n, int rows, int J, int D, int dtype, void* w, void* b,
+                         hipStream_t st) {
+  const dim3 grid((unsigned)(((long)rows * D + CS_COLS - 1) / CS_COLS)), thr(CS_COLS * CS_ROWS);
+  if (dtype == 1)
+    hipLaunchKernelGGL((k_colsum<__bf16>), grid, thr, 0, st, part, n, rows, J, D, (__bf16*)w, (__bf16*)b);
+  else
+    hipLaunchKernelGGL((k_colsum<float>), grid, thr, 0, st, part, n, rows, J, D, (float*)w, (float*)b);
+  return hipGetLastError();
+}
+
+}  // namespace qd

@@ -1,0 +1,438 @@
+// Selective state space scan, forward: prompts (dense or packed) and single tokens.
+//
+//   dt = softplus(raw + bias) or raw;  S_t = exp(dt A) S_{t-1} + dt x_t B_t^T;  y_t = S_t C_t + D x_t
+//
+// per head, S [P][N]; B and C are shared by the H / G heads of a group.  Per
+// chunk of 64 tokens with entry state S, b the prefix sums of dt A,
+// W_ri = exp(b_r - b_i) for i <= r:
+//
+//   Y  = diag(e^b) C S^T + (W o C B^T) diag(dt) X + D X
+//   S' = e^{b_C} S + sum_i e^{b_C - b_i} dt_i x_i B_i^T
+//
+// A workgroup walks the chunks of one (sequence, head, 64 rows of the state)
+// with the state in registers: wave w owns 16 of the rows, as accumulators
+// [n][p], which are operands of the products with C as they stand.  C B^T is
+// formed by rows (wave w: tokens 16 w .. of the chunk) and goes to the other
+// waves through LDS.
+//
+// Few sequences and heads leave most of the chip idle in such a walk.  Then it
+// is cut into segments: a walk without outputs forms each segment's own
+// contribution, these are put together along the sequence, and the walk with
+// outputs starts every segment from its entry.
+#include "qd_ssm.h"
+
+namespace qd {
+
+namespace {
+
+// Zero-filled operand rows outside the matrices make every product exact.
+template <typename E, int NP>
+struct FwdLds {
+  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDC = lds_ld<E>(C), PL = sizeof(E) == 2 ? 2 : 1;
+  E B[C * LDN], Cm[C * LDN], X[C * LDP];
+  E W[PL][C * LDC];
+  Gates g;
+};
+
+template <typename E, int NP>
+__global__ __launch_bounds__(NTHREADS, sizeof(E) == 2 ? 2 : 1) void k_ssm_out(ScanArgs a, long items) {
+  typedef FwdLds<E, NP> L;
+  typedef typename Q4<E>::t q4;
+  __shared__ __attribute__((aligned(16))) L s;
+  constexpr int NB = NP / 16, KN = NP / 32, PL = L::PL;
+  long item;
+  if (!xcd_item(items, item)) return;
+  const int pts = p_tiles(a.P), hp = (int)(item % (a.H * pts)), h = hp / pts, p0 = hp % pts * PT;
+  const long slot = item / (a.H * pts);
+  int n, len, pos;
+  long s0;
+  const bool whole = a.seg == 0;       // one walk a sequence, empty ones included: they hand their state on
+  if (whole) {
+    n = (int)slot;
+    pos = 0;
+    if (!a.q.range(n, s0, len)) return;
+  } else if (!a.q.locate(slot, a.seg, n, s0, len, pos)) {
+    return;
+  }
+  const int end = whole ? len : min(pos + a.seg, len);
+  const int t = threadIdx.x, lane = t & 63, w = wave_id(t), g4 = 4 * (lane >> 4), col = lane & 15;
+  const int cols = min(PT, a.P - p0), grp = h / (a.H / a.G);
+  const E* x = (const E*)a.x + (s0 + pos) * a.ldx + (long)h * a.P + p0;
+  const E* B = (const E*)a.B + (s0 + pos) * a.ldb + (long)grp * a.N;
+  const E* Cm = (const E*)a.C + (s0 + pos) * a.ldc + (long)grp * a.N;
+  const bool vx = vec_rows<E>(x, a.ldx, cols), vb = vec_rows<E>(B, a.ldb, a.N), vc = vec_rows<E>(Cm, a.ldc, a.N);
+  E* y = (E*)a.y + ((s0 + pos) * a.H + h) * (long)a.P + p0;
+  const bool vy = a.P % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(E) - 1)) == 0;
+  const float D = a.D ? a.D[h] : 0.f;
+
+  // state: f4 S[nb] holds n = 16 nb + g4 + j of row p = p0 + 16 w + col
+  const int p = p0 + 16 * w + col;
+  const float* in = whole ? (a.S0 ? a.S0 + ((long)n * a.H + h) * a.P * a.N : nullptr)
+                          : a.entry[0] + (slot * a.H + h) * (long)a.P * a.N;
+  f4 S[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int nn = 16 * nb + g4 + j;
+      S[nb][j] = in && p < a.P && nn < a.N ? in[(long)p * a.N + nn] : 0.f;
+    }
+
+  Stage<E, PT, NTHREADS> rx;
+  Stage<E, NP, NTHREADS> rb, rc;
+  auto fetch = [&](int at) {
+    const int rows = min(C, end - at), d = at - pos;
+    rx.load(x + d * a.ldx, a.ldx, rows, cols, vx, t);
+    rb.load(B + d * a.ldb, a.ldb, rows, a.N, vb, t);
+    rc.load(Cm + d * a.ldc, a.ldc, rows, a.N, vc, t);
+  };
+  if (pos < end) fetch(pos);
+  for (int at = pos; at < end; at += C) {
+    const int rows = min(C, end - at);
+    rx.put(s.X, L::LDP, t);
+    rb.put(s.B, L::LDN, t);
+    rc.put(s.Cm, L::LDN, t);
+    if (w == 0) chunk_gates(s.g, a, s0 + at, rows, h, lane);
+    __syncthreads();
+    if (at + C < end) fetch(at + C);
+
+    // rows r = 16 w + col of W o C B^T diag(dt), as their transposes: accumulator rows are i
+    {
+      Fr<E> c[KN];
+#pragma unroll
+      for (int k = 0; k < KN; ++k) c[k] = row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane);
+      const int r = 16 * w + col;
+      const float hr = s.g.bh[r], lr = s.g.bl[r];
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) {
+        if (ib > (w | 1)) break;       // products take blocks in pairs: the one beside the last is zero
+        f4 v = zero4();
+        if (ib <= w) {
+#pragma unroll
+          for (int k = 0; k < KN; ++k) v = mma(row_frag<E>(s.B, L::LDN, 16 * ib, 32 * k, lane), c[k], v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 16 * ib + g4 + j;
+            v[j] = i <= r ? v[j] * decay(hr, lr, s.g.bh[i], s.g.bl[i]) * s.g.dt[i] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) {
+          const q4 q = narrow<E>(v);
+          *(q4*)(s.W[pl] + r * L::LDC + 16 * ib + g4) = q;
+          if (pl + 1 < PL) v -= widen<E>(q);
+        }
+      }
+    }
+    // Y^T rows p, columns r: from the entry state
+    f4 o[4];
+#pragma unroll
+    for (int rb4 = 0; rb4 < 4; ++rb4) o[rb4] = zero4();
+#pragma unroll
+    for (int k = 0; k < KN; ++k) {
+      const Planes<E, 2> sp = planes<E, 2>(S[2 * k], S[2 * k + 1]);
+#pragma unroll
+      for (int rb4 = 0; rb4 < 4; ++rb4) o[rb4] = mma(sp, row_frag<E>(s.Cm, L::LDN, 16 * rb4, 32 * k, lane), o[rb4]);
+    }
+    Fr<E> xt[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) xt[k] = col_frag<E>(s.X, L::LDP, 32 * k, 16 * w, lane);
+    __syncthreads();
+#pragma unroll
+    for (int rb4 = 0; rb4 < 4; ++rb4) {
+      const int r = 16 * rb4 + col;
+      o[rb4] *= decay(s.g.bh[r], s.g.bl[r], 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k <= rb4 / 2; ++k)
+#pragma unroll
+        for (int pl = PL - 1; pl >= 0; --pl)
+          o[rb4] = mma(xt[k], row_frag<E>(s.W[pl], L::LDC, 16 * rb4, 32 * k, lane), o[rb4]);
+      if (a.D) o[rb4] += D * widen<E>(*(const q4*)(s.X + r * L::LDP + 16 * w + g4));
+      if (r < rows) {
+        const int pc = 16 * w + g4;
+        E* out = y + (long)(at - pos + r) * a.H * a.P + pc;
+        if (vy) {
+          if (pc < cols) *(q4*)out = narrow<E>(o[rb4]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (pc + j < cols) out[j] = fromf<E>(o[rb4][j]);
+        }
+      }
+    }
+    // S' : accumulator rows n, columns p
+    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) S[nb] *= total;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      f4 u, v;
+      quads<E>(xt[k], u, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 32 * k + g4 + j;
+        u[j] *= s.g.dt[i] * decay(he, le, s.g.bh[i], s.g.bl[i]);
+        v[j] *= s.g.dt[i + 16] * decay(he, le, s.g.bh[i + 16], s.g.bl[i + 16]);
+      }
+      const Planes<E, 3> xw = planes<E, 3>(u, v);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane), xw, S[nb]);
+    }
+    __syncthreads();
+  }
+  if (whole && a.Sf && p < a.P) {
+    float* out = a.Sf + (((long)n * a.H + h) * a.P + p) * a.N;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (16 * nb + g4 + j < a.N) out[16 * nb + g4 + j] = S[nb][j];
+  }
+}
+
+// Walk of the state alone (dir 0: S, over x and B from the front), or of its
+// gradient (dir 1: G = dL/dS, over dy and C from the back,
+// G <- e^{b_C} G + sum_r e^{b_r} dy_r C_r^T), over a segment or a whole
+// sequence.  Accumulators [p][n]: f4 S[nb] holds rows p = 16 w + g4 + j of
+// column n = 16 nb + col, which is also the order in `states` and `grads`.
+template <typename E, int NP>
+struct WalkLds {
+  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT);
+  E B[C * LDN], X[C * LDP];
+  Gates g;
+};
+
+template <typename E, int NP>
+__global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items, int dir0, int keep) {
+  typedef WalkLds<E, NP> L;
+  __shared__ __attribute__((aligned(16))) L s;
+  constexpr int NB = NP / 16;
+  long item;
+  if (!xcd_item(items, item)) return;
+  const int dir = dir0 + (int)blockIdx.y;
+  const int pts = p_tiles(a.P), hp = (int)(item % (a.H * pts)), h = hp / pts, p0 = hp % pts * PT;
+  const long slot = item / (a.H * pts);
+  int n, len, pos;
+  long s0;
+  const bool whole = a.seg == 0;
+  if (whole) {
+    n = (int)slot;
+    pos = 0;
+    if (!a.q.range(n, s0, len)) return;
+  } else if (!a.q.locate(slot, a.seg, n, s0, len, pos)) {
+    return;
+  }
+  const int end = whole ? len : min(pos + a.seg, len);
+  const int t = threadIdx.x, lane = t & 63, w = wave_id(t), g4 = 4 * (lane >> 4), col = lane & 15;
+  const int cols = min(PT, a.P - p0), grp = h / (a.H / a.G);
+  const long ldx = dir ? (long)a.H * a.P : a.ldx, ldb = dir ? a.ldc : a.ldb;
+  const E* x = (const E*)(dir ? a.dy : a.x) + (s0 + pos) * ldx + (long)h * a.P + p0;
+  const E* B = (const E*)(dir ? a.C : a.B) + (s0 + pos) * ldb + (long)grp * a.N;
+  const bool vx = vec_rows<E>(x, ldx, cols), vb = vec_rows<E>(B, ldb, a.N);
+
+  // Without `keep` this is a segment's own contribution, from zero; with it the
+  // walk starts from the segment's entry, or the sequence's.
+  const float* ends = dir ? a.dSf : a.S0;
+  const float* in = whole ? (ends ? ends + ((long)n * a.H + h) * a.P * a.N : nullptr)
+                          : keep ? a.entry[dir] + (slot * a.H + h) * (long)a.P * a.N : nullptr;
+  f4 S[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = p0 + 16 * w + g4 + j, nn = 16 * nb + col;
+      S[nb][j] = in && p < a.P && nn < a.N ? in[(long)p * a.N + nn] : 0.f;
+    }
+  double run = 0.0;                      // sum of dt A over the segment
+  const int chunks = (end - pos + C - 1) / C;
+  const long cslot = (a.q.cu ? s0 / C + n : (long)n * ((a.q.T + C - 1) / C)) + pos / C;
+
+  Stage<E, PT, NTHREADS> rx;
+  Stage<E, NP, NTHREADS> rb;
+  auto fetch = [&](int c) {
+    const int rows = min(C, end - pos - c * C);
+    rx.load(x + (long)c * C * ldx, ldx, rows, cols, vx, t);
+    rb.load(B + (long)c * C * ldb, ldb, rows, a.N, vb, t);
+  };
+  if (chunks > 0) fetch(dir ? chunks - 1 : 0);
+  for (int k0 = 0; k0 < chunks; ++k0) {
+    const int c = dir ? chunks - 1 - k0 : k0, rows = min(C, end - pos - c * C);
+    if (keep) {
+      float* out = (dir ? a.grads : a.states) + ((cslot + c) * a.H * pts + hp) * (long)(PT * NP);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) *(f4*)(out + ((w * NB + nb) * 64 + lane) * 4) = S[nb];
+    }
+    rx.put(s.X, L::LDP, t);
+    rb.put(s.B, L::LDN, t);
+    if (w == 0) chunk_gates(s.g, a, s0 + pos + c * C, rows, h, lane);
+    __syncthreads();
+    if (k0 + 1 < chunks) fetch(dir ? c - 1 : c + 1);
+    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
+    run += (double)he + (double)le;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) S[nb] *= total;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const Fr<E> xt = col_frag<E>(s.X, L::LDP, 32 * k, 16 * w, lane);
+      f4 u, v;
+      quads<E>(xt, u, v);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 32 * k + g4 + j, i2 = i + 16;
+        if (dir) {
+          u[j] *= decay(s.g.bh[i], s.g.bl[i], 0.f, 0.f);
+          v[j] *= decay(s.g.bh[i2], s.g.bl[i2], 0.f, 0.f);
+        } else {
+          u[j] *= s.g.dt[i] * decay(he, le, s.g.bh[i], s.g.bl[i]);
+          v[j] *= s.g.dt[i2] * decay(he, le, s.g.bh[i2], s.g.bl[i2]);
+        }
+      }
+      const Planes<E, 3> xw = planes<E, 3>(u, v);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(xw, col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane), S[nb]);
+    }
+    __syncthreads();
+  }
+  float* out = whole ? (dir ? a.dS0 : nullptr) : keep ? nullptr : a.total[dir];
+  if (whole && out) out += ((long)n * a.H + h) * a.P * a.N;
+  else if (out) out += (slot * a.H + h) * (long)a.P * a.N;
+  if (out)
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int p = p0 + 16 * w + g4 + j, nn = 16 * nb + col;
+        if (p < a.P && nn < a.N) out[(long)p * a.N + nn] = S[nb][j];
+      }
+  if (!whole && !keep && dir == dir0 && p0 == 0 && t == 0) a.decay[slot * a.H + h] = (float)run;
+}
+
+// Entries of the segments of each sequence from their own contributions and
+// decays, dir 0 from the front (S0, to Sf), dir 1 from the back (dSf, to dS0).
+__global__ __launch_bounds__(NTHREADS) void k_ssm_compose(ScanArgs a, int dir0) {
+  const int dir = dir0 + (int)blockIdx.z;
+  const long per = (long)a.P * a.N, i = (long)blockIdx.x * NTHREADS + threadIdx.x;
+  const int n = blockIdx.y / a.H, h = blockIdx.y % a.H;
+  int len;
+  long s0;
+  if (i >= per || !a.q.range(n, s0, len)) return;
+  const long base = a.q.cu ? s0 / a.seg + n : (long)n * ((a.q.T + a.seg - 1) / a.seg), at = ((long)n * a.H + h) * per + i;
+  const int k = (len + a.seg - 1) / a.seg;
+  const float* ends = dir ? a.dSf : a.S0;
+  float S = ends ? ends[at] : 0.f;
+  for (int j = 0; j < k; ++j) {
+    const long slot = base + (dir ? k - 1 - j : j), u = slot * a.H + h;
+    a.entry[dir][u * per + i] = S;
+    S = fast_exp(a.decay[u]) * S + a.total[dir][u * per + i];
+  }
+  float* out = dir ? a.dS0 : a.Sf;
+  if (out) out[at] = S;
+}
+
+// One token of N sequences.  A wave owns rows of one head's state, R lanes a
+// row with four consecutive n a lane and piece; the row's sum over n is formed
+// by lane moves.  Bound by the state's bytes, read and written once.
+template <typename E>
+__global__ __launch_bounds__(NTHREADS) void k_ssm_step(ScanArgs a) {
+  constexpr int RPW = 4;                 // rows a wave handles at once: 16 lanes each
+  const int per = (a.P + 4 * RPW - 1) / (4 * RPW);
+  const long unit = blockIdx.x / per;    // (sequence, head)
+  const int n = (int)(unit / a.H), h = (int)(unit % a.H), lane = threadIdx.x & 63, w = wave_id(threadIdx.x);
+  const int p = (int)(blockIdx.x % per) * 4 * RPW + w * RPW + (lane >> 4), l = lane & 15;
+  const int grp = h / (a.H / a.G);
+  const float z = a.dt[unit] + (a.bias ? a.bias[h] : 0.f);
+  const float dt = step_size(z, a.softplus), al = fast_exp(dt * a.A[h]);
+  if (p >= a.P) return;
+  const float x = tof(((const E*)a.x)[n * a.ldx + (long)h * a.P + p]), dx = dt * x;
+  const E* B = (const E*)a.B + n * a.ldb + (long)grp * a.N;
+  const E* Cm = (const E*)a.C + n * a.ldc + (long)grp * a.N;
+  const float* in = a.S0 + (unit * a.P + p) * a.N;
+  float* out = a.Sf + (unit * a.P + p) * a.N;
+  float y = 0.f;
+  if (a.N % 4 == 0 && (((uintptr_t)a.S0 | (uintptr_t)a.Sf) & 15) == 0) {
+    for (int k = 4 * l; k < a.N; k += 64) {
+      f4 S = *(const f4*)(in + k);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        S[j] = al * S[j] + dx * tof(B[k + j]);
+        y += S[j] * tof(Cm[k + j]);
+      }
+      *(f4*)(out + k) = S;
+    }
+  } else {
+    for (int k = l; k < a.N; k += 16) {
+      const float S = al * in[k] + dx * tof(B[k]);
+      y += S * tof(Cm[k]);
+      out[k] = S;
+    }
+  }
+  y = sum16(y);
+  if (l == 0) ((E*)a.y)[unit * a.P + p] = fromf<E>(a.D ? y + a.D[h] * x : y);
+}
+
+long walk_slots(const ScanArgs& a) { return a.seg ? a.q.slots(a.seg) : a.q.N; }
+
+template <typename E, int NP>
+hipError_t out_walk(const ScanArgs& a, hipStream_t st) {
+  const long items = walk_slots(a) * a.H * p_tiles(a.P);
+  if (items == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_ssm_out<E, NP>), dim3(xcd_grid(items)), dim3(NTHREADS), 0, st, a, items);
+  return hipGetLastError();
+}
+
+template <typename E, int NP>
+hipError_t walks(const ScanArgs& a, int dirs, bool chunks, hipStream_t st) {
+  const long items = walk_slots(a) * a.H * p_tiles(a.P);
+  if (items == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_ssm_walk<E, NP>), dim3(xcd_grid(items), dirs == 3 ? 2 : 1), dim3(NTHREADS), 0, st, a, items,
+                     dirs == 2 ? 1 : 0, chunks ? 1 : 0);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_scan_walks(const ScanArgs& a, int dtype, int dirs, bool chunks, hipStream_t st) {
+  if (dtype == 1) return a.N <= 64 ? walks<__bf16, 64>(a, dirs, chunks, st) : walks<__bf16, 128>(a, dirs, chunks, st);
+  return a.N <= 64 ? walks<float, 64>(a, dirs, chunks, st) : walks<float, 128>(a, dirs, chunks, st);
+}
+
+hipError_t launch_scan_compose(const ScanArgs& a, int dirs, hipStream_t st) {
+  const long per = (long)a.P * a.N;
+  if (a.q.N == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_ssm_compose, dim3((unsigned)((per + NTHREADS - 1) / NTHREADS), (unsigned)(a.q.N * a.H), dirs == 3 ? 2 : 1),
+                     dim3(NTHREADS), 0, st, a, dirs == 2 ? 1 : 0);
+  return hipGetLastError();
+}
+
+// A walk takes about 2 us a chunk whatever runs beside it, up to two
+// workgroups a CU; so sequences are cut until that many run, into no less than
+// four chunks (a segment costs a second walk without outputs, and its state).
+int scan_segment(const Seqs& q, int H, int P, int dirs) {
+  const long tokens = q.cu ? q.T : (long)q.N * q.T, want = 2L * device_cu_count();
+  const long units = (long)q.N * H * p_tiles(P) * dirs;
+  if (units <= 0 || units >= want / 2) return 0;
+  const long slots = want / ((long)H * p_tiles(P) * dirs);       // segments to have in all
+  long chunks = (tokens / (slots > 0 ? slots : 1) + C - 1) / C;
+  if (chunks < 4) chunks = 4;
+  return q.T <= chunks * C ? 0 : (int)(chunks * C);
+}
+
+hipError_t launch_scan_fwd(const ScanArgs& a, int dtype, hipStream_t st) {
+  if (a.seg) {
+    hipError_t e = launch_scan_walks(a, dtype, 1, false, st);
+    if (e == hipSuccess) e = launch_scan_compose(a, 1, st);
+    if (e != hipSuccess) return e;
+  }
+  if (dtype == 1) return a.N <= 64 ? out_walk<__bf16, 64>(a, st) : out_walk<__bf16, 128>(a, st);
+  return a.N <= 64 ? out_walk<float, 64>(a, st) : out_walk<float, 128>(a, st);
+}
+
+hipError_t launch_scan_step(const ScanArgs& a, int dtype, hipStream_t st) {
+  const long blocks = (long)a.q.N * a.H * ((a.P + 15) / 16);
+  if (blocks == 0) return hipSuccess;
+  if (dtype == 1) hipLaunchKernelGGL((k_ssm_step<__bf16>), dim3((unsigned)blocks), dim3(NTHREADS), 0, st, a);
+  else hipLaunchKernelGGL((k_ssm_step<float>), dim3((unsigned)blocks), dim3(NTHREADS), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace qd

@@ -57,12 +57,12 @@ int check_scan(const qd::Seqs& q, int32_t H, int32_t G, int32_t P, int32_t Ns, i
   return QDELTA_OK;
 }
 
-// Workspace of a scan: segments (contributions and entries a direction, and
+// Workspace of a scan: the chunks' gates; segments (contributions and entries a direction, and
 // decays), and for the backward the chunks' states and gradients, the heads'
 // sums and the splits' shares of dB and dC.
 struct ScanWs {
   int seg = 0, splits = 1;
-  size_t entry[2] = {0, 0}, total[2] = {0, 0}, decay = 0, states = 0, grads = 0, partB = 0, partC = 0, sums = 0, bytes = 0;
+  size_t entry[2] = {0, 0}, total[2] = {0, 0}, decay = 0, states = 0, grads = 0, partB = 0, partC = 0, sums = 0, gates = 0, bytes = 0;
 };
 ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd) {
   ScanWs w;
@@ -71,6 +71,7 @@ ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd) {
     w.bytes += (n + 255) & ~size_t(255);
     return at;
   };
+  w.gates = take((size_t)q.slots(qd::C) * H * qd::GATES * 4);
   w.seg = qd::scan_segment(q, H, P, bwd ? 2 : 1);
   if (w.seg) {
     const size_t heads = (size_t)q.slots(w.seg) * H;
@@ -108,6 +109,7 @@ void bind_ws(qd::ScanArgs& a, const ScanWs& w, void* ws) {
   a.partB = at(w.partB);
   a.partC = at(w.partC);
   a.sums = at(w.sums);
+  a.gates = at(w.gates);
 }
 
 // Fills the arguments that all scan entry points share and checks them.

@@ -162,6 +162,7 @@ struct ScanArgs {
   int splits;                      // workgroups that share a chunk's heads
   float *partB, *partC;            // [split][tokens][G][N] where splits > 1
   float* sums;                     // [chunk slot][H][4]: dA, dD, dbias
+  float* gates;                    // [chunk slot][H] Gates
 };
 
 __host__ __device__ inline int p_tiles(int P) { return (P + PT - 1) / PT; }
@@ -234,27 +235,22 @@ __device__ inline double wave_incl_scan64(double x) {
   return x;
 }
 
-// Time steps and prefix sums b of dt A of a chunk, one token a lane of one
-// wave.  b is kept as two floats: what counts are differences b_r - b_i, and a
-// token that wipes the state (dt A = -10^4) would leave a single float's
-// differences after it off by 6e-4.
+// Time steps and prefix sums b of dt A of a chunk, formed once for all kernels
+// of a call ([chunk slot][H] of them).  b is kept as two floats: what counts
+// are differences b_r - b_i, and a token that wipes the state (dt A = -10^4)
+// would leave a single float's differences after it off by 6e-4.  Tokens past
+// the chunk's end have dt = 0, so that b stays where it is.
 struct Gates {
   float dt[C], bh[C], bl[C];
 };
+constexpr int GATES = 3 * C;
 __device__ inline float step_size(float z, int softplus) {
   return softplus ? fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) : z;
-}
-__device__ inline void chunk_gates(Gates& g, const ScanArgs& a, long t0, int len, int h, int lane) {
-  float dt = 0.f;
-  if (lane < len) dt = step_size(a.dt[(t0 + lane) * a.H + h] + (a.bias ? a.bias[h] : 0.f), a.softplus);
-  const double b = wave_incl_scan64((double)dt * (double)a.A[h]);
-  g.dt[lane] = dt;
-  g.bh[lane] = (float)b;
-  g.bl[lane] = (float)(b - (double)(float)b);
 }
 // exp(b_r - b_i); exp(b_r) with zeros for b_i.
 __device__ inline float decay(float hr, float lr, float hi, float li) { return fast_exp((hr - hi) + (lr - li)); }
 
+hipError_t launch_scan_gates(const ScanArgs& a, hipStream_t st);
 hipError_t launch_scan_fwd(const ScanArgs& a, int dtype, hipStream_t st);
 hipError_t launch_scan_bwd(const ScanArgs& a, int dtype, hipStream_t st);
 hipError_t launch_scan_step(const ScanArgs& a, int dtype, hipStream_t st);

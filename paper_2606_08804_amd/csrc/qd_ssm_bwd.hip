@@ -19,7 +19,8 @@
 // The states S and gradients G of all chunks come from two walks (one launch);
 // then chunks are independent.  A workgroup takes a chunk and loops over the
 // heads of a group (or a share of them: `splits`, whose dB and dC are then
-// summed in order), with K and the group's dB and dC in registers:
+// summed in order), with K and the group's dB and dC in registers.  Waves 0 to
+// 3 form dC (S, E^T) and G B^T, waves 4 to 7 dB and dX (G, E); of each four
 //   wave w, tokens 16 w ..      the products over the chunk's tokens, from
 //                               E and E^T as they stand in the accumulators;
 //   wave w, a quarter of n      the products with S and G, whose operands are
@@ -46,6 +47,19 @@ struct BwdLds {
   float mcol[C], diag[C], err[C], srow[4][C], gcol[4][C], sg[4];
 };
 
+// Keeps the scheduler from drawing the loads of one phase of a turn into the
+// phase before, where all registers are taken.
+__device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
+
+// The lane number as a value the compiler cannot trace: what is formed from it
+// (LDS addresses, masks of the triangles) is formed again every turn of the
+// loop over heads instead of being kept in registers, which are all taken
+// (hoisted, 130 such values went to scratch memory and back).
+__device__ inline int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Sum over the four lane groups (the rows of an accumulator's columns).
 __device__ inline float groups_sum(float x) {
   x += __shfl_xor(x, 16, 64);
@@ -60,11 +74,11 @@ __device__ inline float before_lane(float x, int lane) {
 }
 
 template <typename E, int NP>
-__global__ __launch_bounds__(NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items) {
+__global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items) {
   typedef BwdLds<E, NP> L;
   typedef typename Q4<E>::t q4;
   __shared__ __attribute__((aligned(16))) L s;
-  constexpr int NB = NP / 16, KN = NP / 32, NQ = NB / 4, PL = L::PL;
+  constexpr int NB = NP / 16, KN = NP / 32, NQ = NB / 4, PL = L::PL, NT = 2 * NTHREADS;
   long item;
   if (!xcd_item(items, item)) return;
   const int per = a.G * a.splits, grp = (int)(item % per) / a.splits, split = (int)(item % a.splits);
@@ -72,13 +86,15 @@ __global__ __launch_bounds__(NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items)
   int n, len, pos;
   long s0;
   if (!a.q.locate(slot, C, n, s0, len, pos)) return;
-  const int rows = min(C, len - pos), t = threadIdx.x, lane = t & 63, w = wave_id(t), g4 = 4 * (lane >> 4), col = lane & 15;
+  const int rows = min(C, len - pos), t = threadIdx.x, lane0 = t & 63, lane = lane0, wave = wave_id(t), w = wave & 3;
+  const int g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;     // this lane's token in the products over tokens
   const long t0 = s0 + pos;
   const int pts = p_tiles(a.P), hg = a.H / a.G;
   const int h0 = grp * hg + hg * split / a.splits, h1 = grp * hg + hg * (split + 1) / a.splits;
+  const int turns = (h1 - h0) * pts;
 
   {
-    Stage<E, NP, NTHREADS> rb, rc;
+    Stage<E, NP, NT> rb, rc;
     const E* B = (const E*)a.B + t0 * a.ldb + (long)grp * a.N;
     const E* Cm = (const E*)a.C + t0 * a.ldc + (long)grp * a.N;
     rb.load(B, a.ldb, rows, a.N, vec_rows<E>(B, a.ldb, a.N), t);
@@ -86,147 +102,142 @@ __global__ __launch_bounds__(NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items)
     rb.put(s.B, L::LDN, t);
     rc.put(s.Cm, L::LDN, t);
   }
-  Stage<E, PT, NTHREADS> rx, ry;
-  auto fetch = [&](int h, int pt) {
-    const int cols = min(PT, a.P - pt * PT);
+  Stage<E, PT, NT> rx, ry;
+  float rg = 0.f;
+  auto fetch = [&](int turn) {
+    const int h = h0 + turn / pts, pt = turn % pts, cols = min(PT, a.P - pt * PT);
     const E* x = (const E*)a.x + t0 * a.ldx + (long)h * a.P + pt * PT;
     const E* dy = (const E*)a.dy + (t0 * a.H + h) * a.P + pt * PT;
     rx.load(x, a.ldx, rows, cols, vec_rows<E>(x, a.ldx, cols), t);
     ry.load(dy, (long)a.H * a.P, rows, cols, vec_rows<E>(dy, (long)a.H * a.P, cols), t);
+    if (t < GATES) rg = a.gates[(slot * a.H + h) * GATES + t];
   };
-  fetch(h0, 0);
-  __syncthreads();
-
-  // K: of columns i = 16 w + col (accumulator rows r), and of rows r = 16 w + col (accumulator rows i)
-  f4 kc[4], kr[4];
+  auto put = [&]() {
+    rx.put(s.X, L::LDP, t);
+    ry.put(s.dY, L::LDP, t);
+    if (t < GATES) ((float*)&s.g)[t] = rg;
+  };
+  // this wave's quarter of a state or gradient: f4 [pb][nq] holds rows p = 16 pb + g4 + j of column n
+  auto quarter = [&](f4(&v)[4][NQ], const float* from, int turn, int lane) {
+    const float* src = from + (slot * a.H * pts + (long)h0 * pts + turn) * (long)(PT * NP);
 #pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    kc[b] = kr[b] = zero4();
-    if (b >= w)
+    for (int pb = 0; pb < 4; ++pb)
 #pragma unroll
-      for (int k = 0; k < KN; ++k)
-        kc[b] = mma(row_frag<E>(s.Cm, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.B, L::LDN, 16 * w, 32 * k, lane), kc[b]);
-    if (b <= w)
+      for (int q = 0; q < NQ; ++q) v[pb][q] = *(const f4*)(src + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
+  };
+  // dB or dC of the chunk: [n][token] accumulators of this lane's token over all n, and of all tokens over a quarter of n
+  const long gn = (long)a.G * a.N;
+  auto half = [&](const f4(&v)[NQ][4]) {
 #pragma unroll
-      for (int k = 0; k < KN; ++k)
-        kr[b] = mma(row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane), kr[b]);
-  }
-  // dC^T, dB^T [n][token]: tokens 16 w + col of all n, and all tokens of this wave's quarter of n
-  f4 dct[NB], dbt[NB], dcn[NQ][4], dbn[NQ][4];
+    for (int q = 0; q < NQ; ++q)
 #pragma unroll
-  for (int b = 0; b < NB; ++b) dct[b] = dbt[b] = zero4();
+      for (int b = 0; b < 4; ++b) *(f4*)(s.sum + (16 * b + col) * L::LDS_ + 16 * (w * NQ + q) + g4) = v[q][b];
+  };
+  auto write = [&](const f4(&v)[NB], void* whole, float* part) {
+    if (own >= rows) return;
+    const bool vq = a.N % 4 == 0 && ((uintptr_t)whole & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
-  for (int b = 0; b < NQ; ++b)
+    for (int b = 0; b < NB; ++b) {
+      const int nn = 16 * b + g4;
+      const f4 x = v[b] + *(const f4*)(s.sum + own * L::LDS_ + nn);
+      const long at = (t0 + own) * gn + (long)grp * a.N + nn;
+      if (a.splits > 1) {
+        const long tokens = a.q.cu ? a.q.T : (long)a.q.N * a.q.T;
+        float* out = part + split * tokens * gn + at;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) dcn[b][k] = dbn[b][k] = zero4();
-
-  for (int h = h0; h < h1; ++h) {
-    for (int pt = 0; pt < pts; ++pt) {
-      const bool first = pt == 0;
-      rx.put(s.X, L::LDP, t);
-      ry.put(s.dY, L::LDP, t);
-      if (first && w == 0) chunk_gates(s.g, a, t0, rows, h, lane);
-      const long tile = ((slot * a.H + h) * pts + pt) * (long)(PT * NP);
-      // this wave's quarter of S and G: f4 [pb][nq] holds rows p = 16 pb + g4 + j of column n
-      f4 S[4][NQ], G[4][NQ];
+        for (int j = 0; j < 4; ++j)
+          if (nn + j < a.N) out[j] = x[j];
+      } else if (vq) {
+        if (nn < a.N) *(q4*)((E*)whole + at) = narrow<E>(x);
+      } else {
 #pragma unroll
-      for (int pb = 0; pb < 4; ++pb)
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          const long at = tile + ((pb * NB + w * NQ + q) * 64 + lane) * 4;
-          S[pb][q] = *(const f4*)(a.states + at);
-          G[pb][q] = *(const f4*)(a.grads + at);
-        }
-      if (pt + 1 < pts) fetch(h, pt + 1);
-      else if (h + 1 < h1) fetch(h + 1, 0);
-      __syncthreads();
-      const float he = s.g.bh[C - 1], le = s.g.bl[C - 1];
-
-      float sg = 0.f;
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const int nn = 16 * (w * NQ + q) + col;
-#pragma unroll
-        for (int pb = 0; pb < 4; ++pb) {
-          f4 v = G[pb][q];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sg += v[j] * S[pb][q][j];
-#pragma unroll
-          for (int pl = 0; pl < PL; ++pl) {
-            const q4 x = narrow<E>(v);
-            *(q4*)(s.G[pl] + nn * L::LDP + 16 * pb + g4) = x;
-            if (pl + 1 < PL) v -= widen<E>(x);
-          }
-        }
+        for (int j = 0; j < 4; ++j)
+          if (nn + j < a.N) ((E*)whole)[at + j] = fromf<E>(x[j]);
       }
-      sg = groups_sum(sum16(sg));
-      if (lane == 0) s.sg[w] = (first ? 0.f : s.sg[w]) + sg;
+    }
+  };
+  fetch(0);
 
-      // products with S and G over this wave's quarter of n
+  if (wave < 4) {
+    f4 S[4][NQ], kr[4], dct[NB], dcn[NQ][4];
+    quarter(S, a.states, 0, lane);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) dct[b] = zero4();
+#pragma unroll
+    for (int b = 0; b < NQ; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dcn[b][k] = zero4();
+    __syncthreads();
+    // K of rows r = own: accumulator rows are i
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      kr[b] = zero4();
+      if (b <= w)
+#pragma unroll
+        for (int k = 0; k < KN; ++k)
+          kr[b] = mma(row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane), kr[b]);
+    }
+    for (int turn = 0; turn < turns; ++turn) {
+      const bool first = turn % pts == 0;
+      const int lane = fresh(lane0), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+      put();
+      __syncthreads();
+      if (turn + 1 < turns) fetch(turn + 1);
+      const float he = s.g.bh[C - 1], le = s.g.bl[C - 1];
+      // e^{b_r} S^T dy_r over this wave's quarter of n
       {
-        float sr[4] = {}, gc[4] = {};
+        float sr[4] = {};
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           const int n0 = 16 * (w * NQ + q) + g4;
-          f4 u[4], v[4];
+          f4 u[4];
 #pragma unroll
-          for (int b = 0; b < 4; ++b) u[b] = v[b] = zero4();
+          for (int b = 0; b < 4; ++b) u[b] = zero4();
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const Planes<E, 3> sp = planes<E, 3>(S[2 * k][q], S[2 * k + 1][q]);
-            const Planes<E, 3> gp = planes<E, 3>(G[2 * k][q], G[2 * k + 1][q]);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              u[b] = mma(sp, row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), u[b]);
-              v[b] = mma(gp, row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), v[b]);
-            }
+            for (int b = 0; b < 4; ++b) u[b] = mma(sp, row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), u[b]);
           }
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             const int r = 16 * b + col;
             u[b] *= decay(s.g.bh[r], s.g.bl[r], 0.f, 0.f);
-            v[b] *= decay(he, le, s.g.bh[r], s.g.bl[r]);
-            const f4 c = widen<E>(*(const q4*)(s.Cm + r * L::LDN + n0)), bb = widen<E>(*(const q4*)(s.B + r * L::LDN + n0));
+            const f4 c = widen<E>(*(const q4*)(s.Cm + r * L::LDN + n0));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              sr[b] += c[j] * u[b][j];
-              gc[b] += bb[j] * v[b][j];
-            }
+            for (int j = 0; j < 4; ++j) sr[b] += c[j] * u[b][j];
             dcn[q][b] += u[b];
-            dbn[q][b] += s.g.dt[r] * v[b];
           }
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           sr[b] = groups_sum(sr[b]);
-          gc[b] = groups_sum(gc[b]);
-          if (g4 == 0) {
-            const int r = 16 * b + col;
-            s.srow[w][r] = (first ? 0.f : s.srow[w][r]) + sr[b];
-            s.gcol[w][r] = (first ? 0.f : s.gcol[w][r]) + gc[b];
-          }
+          if (g4 == 0) s.srow[w][16 * b + col] = (first ? 0.f : s.srow[w][16 * b + col]) + sr[b];
         }
       }
-
-      // dC of tokens r = 16 w + col: accumulator rows i of E^T
+      phase();
+      if (turn + 1 < turns) quarter(S, a.states, turn + 1, lane);
+      phase();
+      // W E diag(dt) of rows r = own: accumulator rows are i
+      f4 e[4], md = zero4();
       {
-        const int r = 16 * w + col;
-        const float hr = s.g.bh[r], lr = s.g.bl[r];
-        f4 e[4], md = zero4();
+        const float hr = s.g.bh[own], lr = s.g.bl[own];
         float before = 0.f;                // sum of M_ri over the blocks i < 16 w
+        Fr<E> yf[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * w, 32 * k, lane);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           e[b] = zero4();
           if (b > w) continue;
 #pragma unroll
-          for (int k = 0; k < 2; ++k)
-            e[b] = mma(row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), row_frag<E>(s.dY, L::LDP, 16 * w, 32 * k, lane), e[b]);
+          for (int k = 0; k < 2; ++k) e[b] = mma(row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), yf[k], e[b]);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int i = 16 * b + g4 + j;
-            const float f = i <= r ? e[b][j] * decay(hr, lr, s.g.bh[i], s.g.bl[i]) * s.g.dt[i] : 0.f;
+            const float f = i <= own ? e[b][j] * decay(hr, lr, s.g.bh[i], s.g.bl[i]) * s.g.dt[i] : 0.f;
             e[b][j] = f;
-            const float m = i < r ? f * kr[b][j] : 0.f;
+            const float m = i < own ? f * kr[b][j] : 0.f;
             if (b == w) {
               md[j] = m;
             } else {
@@ -235,76 +246,21 @@ __global__ __launch_bounds__(NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items)
               if (col == 0) s.cs[w - 1][i] = (first ? 0.f : s.cs[w - 1][i]) + c;
             }
           }
+          phase();
         }
-        // sum over r >= t in this block and all i < t, t = 16 w + col: (M V)_rt with V_it = [i < t] as a product,
-        // the blocks before as one more column, then the rows r >= t
-        {
-          before = groups_sum(before);
-          f4 v = __builtin_amdgcn_mfma_f32_16x16x4f32(g4 == 0 ? before : 0.f, 1.f, zero4(), 0, 0, 0);
+        // sum over r >= t in this block and all i < t, t = own: (M V)_rt with V_it = [i < t] as a product, the
+        // blocks before as one more column, then the rows r >= t
+        before = groups_sum(before);
+        f4 v = __builtin_amdgcn_mfma_f32_16x16x4f32(g4 == 0 ? before : 0.f, 1.f, zero4(), 0, 0, 0);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x4f32(md[j], g4 + j < col ? 1.f : 0.f, v, 0, 0, 0);
-          float f = 0.f;
+        for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x4f32(md[j], g4 + j < col ? 1.f : 0.f, v, 0, 0, 0);
+        float f = 0.f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f += g4 + j >= col ? v[j] : 0.f;
-          f = groups_sum(f);
-          if (g4 == 0) s.fd[r] = (first ? 0.f : s.fd[r]) + f;
-        }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (2 * k > w) break;
-          const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) dct[b] = mma(col_frag<E>(s.B, L::LDN, 32 * k, 16 * b, lane), ep, dct[b]);
-        }
+        for (int j = 0; j < 4; ++j) f += g4 + j >= col ? v[j] : 0.f;
+        f = groups_sum(f);
+        if (g4 == 0) s.fd[own] = (first ? 0.f : s.fd[own]) + f;
       }
-      // dB and dX of tokens i = 16 w + col: accumulator rows r of E
-      f4 xacc[4];
-      {
-        const int i = 16 * w + col;
-        const float hi = s.g.bh[i], li = s.g.bl[i], dt = s.g.dt[i];
-        float mcol = 0.f, diag = 0.f, err = 0.f;
-        f4 e[4], wk[4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          e[b] = wk[b] = zero4();
-          if (b < w) continue;
-#pragma unroll
-          for (int k = 0; k < 2; ++k)
-            e[b] = mma(row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), row_frag<E>(s.X, L::LDP, 16 * w, 32 * k, lane), e[b]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int r = 16 * b + g4 + j;
-            const float wt = r >= i ? decay(s.g.bh[r], s.g.bl[r], hi, li) : 0.f;
-            const float ev = r >= i ? e[b][j] : 0.f, f = ev * wt;
-            mcol += r > i ? f * kc[b][j] : 0.f;
-            diag += r == i ? ev * kc[b][j] : 0.f;
-            err += r == i ? ev : 0.f;
-            e[b][j] = f * dt;
-            wk[b][j] = r >= i ? wt * kc[b][j] : 0.f;
-          }
-        }
-        mcol = groups_sum(mcol);
-        diag = groups_sum(diag);
-        err = groups_sum(err);
-        if (g4 == 0) {
-          s.mcol[i] = (first ? 0.f : s.mcol[i]) + mcol;
-          s.diag[i] = (first ? 0.f : s.diag[i]) + diag;
-          s.err[i] = (first ? 0.f : s.err[i]) + err;
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) xacc[b] = zero4();
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          if (2 * k + 1 < w) continue;
-          const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) dbt[b] = mma(col_frag<E>(s.Cm, L::LDN, 32 * k, 16 * b, lane), ep, dbt[b]);
-          const Planes<E, 2> wp = planes<E, 2>(wk[2 * k], wk[2 * k + 1]);
-#pragma unroll
-          for (int b = 0; b < 4; ++b) xacc[b] = mma(col_frag<E>(s.dY, L::LDP, 32 * k, 16 * b, lane), wp, xacc[b]);
-        }
-      }
-      __syncthreads();                     // G is in LDS
+      phase();
       // rows p = 16 w .. of G B^T for all tokens, to the waves that own them
       {
         f4 v[4];
@@ -329,96 +285,210 @@ __global__ __launch_bounds__(NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items)
         }
       }
       __syncthreads();
-      {
-        const int i = 16 * w + col, cols = min(PT, a.P - pt * PT);
-        const float dt = s.g.dt[i], D = a.D ? a.D[h] : 0.f;
-        E* out = (E*)a.dx + ((t0 + i) * a.H + h) * (long)a.P + pt * PT;
-        const bool vo = a.P % 4 == 0 && ((uintptr_t)a.dx & (4 * sizeof(E) - 1)) == 0;
-        if (i < rows)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const int p = 16 * b + g4;
-            f4 v = dt * (xacc[b] + *(const f4*)(s.dX + i * L::LDT + p));
-            if (a.D) v += D * widen<E>(*(const q4*)(s.dY + i * L::LDP + p));
-            if (vo) {
-              if (p < cols) *(q4*)(out + p) = narrow<E>(v);
-            } else {
+      for (int k = 0; k < 2; ++k) {
+        if (2 * k > w) break;
+        const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                if (p + j < cols) out[p + j] = fromf<E>(v[j]);
-            }
-          }
-      }
-      // the time step's gradient and the head's sums, a token a lane
-      if (pt == pts - 1 && w == 0) {
-        const int r = lane;
-        const float dt = s.g.dt[r], A = a.A[h];
-        const float srow = (s.srow[0][r] + s.srow[1][r]) + (s.srow[2][r] + s.srow[3][r]);
-        const float gcol = (s.gcol[0][r] + s.gcol[1][r]) + (s.gcol[2][r] + s.gcol[3][r]);
-        float dl = ((s.sg[0] + s.sg[1]) + (s.sg[2] + s.sg[3])) * decay(he, le, 0.f, 0.f);
-        dl += lane_from(wave_incl_scan_dpp(lane_from(srow, 63 - lane)), 63 - lane);        // over r >= t
-        dl += before_lane(dt * gcol, lane) + s.fd[r];                                      // over i < t
-#pragma unroll
-        for (int b = 1; b < 4; ++b) {
-          const float c = before_lane(r < 16 * b ? s.cs[b - 1][r] : 0.f, lane);
-          dl += r < 16 * b ? c : 0.f;
-        }
-        const float ddt = s.mcol[r] + s.diag[r] + gcol + A * dl;
-        float raw = ddt;
-        const bool in = r < rows;
-        if (a.softplus) {
-          const float z = in ? a.dt[(t0 + r) * a.H + h] + (a.bias ? a.bias[h] : 0.f) : 0.f;
-          raw *= 1.f / (1.f + expf(-z));
-        }
-        if (in) a.ddt[(t0 + r) * a.H + h] = raw;
-        float sa = in ? dt * dl : 0.f, sd = in ? s.err[r] : 0.f, sb = in ? raw : 0.f;
-        sa = groups_sum(sum16(sa));
-        sd = groups_sum(sum16(sd));
-        sb = groups_sum(sum16(sb));
-        if (lane == 0) *(f4*)(a.sums + (slot * a.H + h) * 4) = f4{sa, sd, sb, 0.f};
+        for (int b = 0; b < NB; ++b) dct[b] = mma(col_frag<E>(s.B, L::LDN, 32 * k, 16 * b, lane), ep, dct[b]);
       }
       __syncthreads();
     }
+    half(dcn);
+    __syncthreads();
+    write(dct, a.dC, a.partC);
+    __syncthreads();
+    __syncthreads();
+    return;
   }
 
-  // dC, then dB: the two halves meet in LDS
-  const long gn = (long)a.G * a.N;
-  const bool vq = a.N % 4 == 0;
+  f4 G[4][NQ], kc[4], dbt[NB], dbn[NQ][4];
+  quarter(G, a.grads, 0, lane);
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const f4(&half)[NQ][4] = which ? dbn : dcn;
-    const f4(&mine)[NB] = which ? dbt : dct;
+  for (int b = 0; b < NB; ++b) dbt[b] = zero4();
 #pragma unroll
-    for (int q = 0; q < NQ; ++q)
+  for (int b = 0; b < NQ; ++b)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) *(f4*)(s.sum + (16 * b + col) * L::LDS_ + 16 * (w * NQ + q) + g4) = half[q][b];
+    for (int k = 0; k < 4; ++k) dbn[b][k] = zero4();
+  __syncthreads();
+  // K of columns i = own: accumulator rows are r
+#pragma unroll
+  for (int b = 0; b < 4; ++b) {
+    kc[b] = zero4();
+    if (b >= w)
+#pragma unroll
+      for (int k = 0; k < KN; ++k)
+        kc[b] = mma(row_frag<E>(s.Cm, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.B, L::LDN, 16 * w, 32 * k, lane), kc[b]);
+  }
+  for (int turn = 0; turn < turns; ++turn) {
+    const bool first = turn % pts == 0;
+    const int h = h0 + turn / pts, pt = turn % pts;
+    const int lane = fresh(lane0), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+    put();
+    float sg = 0.f;
+    {
+      const float* S = a.states + (slot * a.H * pts + (long)h0 * pts + turn) * (long)(PT * NP);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        const int nn = 16 * (w * NQ + q) + col;
+#pragma unroll
+        for (int pb = 0; pb < 4; ++pb) {
+          f4 v = G[pb][q];
+          const f4 sv = *(const f4*)(S + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sg += v[j] * sv[j];
+#pragma unroll
+          for (int pl = 0; pl < PL; ++pl) {
+            const q4 x = narrow<E>(v);
+            *(q4*)(s.G[pl] + nn * L::LDP + 16 * pb + g4) = x;
+            if (pl + 1 < PL) v -= widen<E>(x);
+          }
+        }
+        phase();
+      }
+    }
+    sg = groups_sum(sum16(sg));
+    if (lane == 0) s.sg[w] = (first ? 0.f : s.sg[w]) + sg;
     __syncthreads();
-    const int r = 16 * w + col;
-    if (r < rows)
+    if (turn + 1 < turns) fetch(turn + 1);
+    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1];
+    // e^{b_C - b_i} G^T x_i over this wave's quarter of n
+    {
+      float gc[4] = {};
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int nn = 16 * b + g4;
-        const f4 v = mine[b] + *(const f4*)(s.sum + r * L::LDS_ + nn);
-        const long at = (t0 + r) * gn + (long)grp * a.N + nn;
-        if (a.splits > 1) {
-          const long tokens = a.q.cu ? a.q.T : (long)a.q.N * a.q.T;
-          float* out = (which ? a.partB : a.partC) + split * tokens * gn + at;
+      for (int q = 0; q < NQ; ++q) {
+        const int n0 = 16 * (w * NQ + q) + g4;
+        f4 v[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (nn + j < a.N) out[j] = v[j];
-        } else {
-          E* out = (E*)(which ? a.dB : a.dC) + at;
-          if (vq && ((uintptr_t)out & (4 * sizeof(E) - 1)) == 0) {
-            if (nn < a.N) *(q4*)out = narrow<E>(v);
+        for (int b = 0; b < 4; ++b) v[b] = zero4();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const Planes<E, 3> gp = planes<E, 3>(G[2 * k][q], G[2 * k + 1][q]);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) v[b] = mma(gp, row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), v[b]);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int i = 16 * b + col;
+          v[b] *= decay(he, le, s.g.bh[i], s.g.bl[i]);
+          const f4 bb = widen<E>(*(const q4*)(s.B + i * L::LDN + n0));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) gc[b] += bb[j] * v[b][j];
+          dbn[q][b] += s.g.dt[i] * v[b];
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        gc[b] = groups_sum(gc[b]);
+        if (g4 == 0) s.gcol[w][16 * b + col] = (first ? 0.f : s.gcol[w][16 * b + col]) + gc[b];
+      }
+    }
+    phase();
+    if (turn + 1 < turns) quarter(G, a.grads, turn + 1, lane);
+    phase();
+    // W E and W K of columns i = own: accumulator rows are r
+    f4 xacc[4];
+    const float dt = s.g.dt[own];
+    {
+      const float hi = s.g.bh[own], li = s.g.bl[own];
+      float mcol = 0.f, diag = 0.f, err = 0.f;
+      f4 e[4], wk[4];
+      Fr<E> xf[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) xf[k] = row_frag<E>(s.X, L::LDP, 16 * w, 32 * k, lane);
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        e[b] = wk[b] = zero4();
+        if (b < w) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) e[b] = mma(row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), xf[k], e[b]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int r = 16 * b + g4 + j;
+          const float wt = r >= own ? decay(s.g.bh[r], s.g.bl[r], hi, li) : 0.f;
+          const float ev = r >= own ? e[b][j] : 0.f, f = ev * wt;
+          mcol += r > own ? f * kc[b][j] : 0.f;
+          diag += r == own ? ev * kc[b][j] : 0.f;
+          err += r == own ? ev : 0.f;
+          e[b][j] = f * dt;
+          wk[b][j] = r >= own ? wt * kc[b][j] : 0.f;
+        }
+        phase();
+      }
+      mcol = groups_sum(mcol);
+      diag = groups_sum(diag);
+      err = groups_sum(err);
+      if (g4 == 0) {
+        s.mcol[own] = (first ? 0.f : s.mcol[own]) + mcol;
+        s.diag[own] = (first ? 0.f : s.diag[own]) + diag;
+        s.err[own] = (first ? 0.f : s.err[own]) + err;
+      }
+      phase();
+#pragma unroll
+      for (int b = 0; b < 4; ++b) xacc[b] = zero4();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if (2 * k + 1 < w) continue;
+        const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) dbt[b] = mma(col_frag<E>(s.Cm, L::LDN, 32 * k, 16 * b, lane), ep, dbt[b]);
+        const Planes<E, 2> wp = planes<E, 2>(wk[2 * k], wk[2 * k + 1]);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) xacc[b] = mma(col_frag<E>(s.dY, L::LDP, 32 * k, 16 * b, lane), wp, xacc[b]);
+      }
+    }
+    __syncthreads();
+    {
+      const int cols = min(PT, a.P - pt * PT);
+      const float D = a.D ? a.D[h] : 0.f;
+      E* out = (E*)a.dx + ((t0 + own) * a.H + h) * (long)a.P + pt * PT;
+      const bool vo = a.P % 4 == 0 && ((uintptr_t)a.dx & (4 * sizeof(E) - 1)) == 0;
+      if (own < rows)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const int p = 16 * b + g4;
+          f4 v = dt * (xacc[b] + *(const f4*)(s.dX + own * L::LDT + p));
+          if (a.D) v += D * widen<E>(*(const q4*)(s.dY + own * L::LDP + p));
+          if (vo) {
+            if (p < cols) *(q4*)(out + p) = narrow<E>(v);
           } else {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (nn + j < a.N) out[j] = fromf<E>(v[j]);
+              if (p + j < cols) out[p + j] = fromf<E>(v[j]);
           }
         }
+    }
+    // the time step's gradient and the head's sums, a token a lane, on the wave with the fewest products
+    if (pt == pts - 1 && w == 3) {
+      const int r = lane;
+      const float step = s.g.dt[r], A = a.A[h];
+      const float srow = (s.srow[0][r] + s.srow[1][r]) + (s.srow[2][r] + s.srow[3][r]);
+      const float gcol = (s.gcol[0][r] + s.gcol[1][r]) + (s.gcol[2][r] + s.gcol[3][r]);
+      float dl = ((s.sg[0] + s.sg[1]) + (s.sg[2] + s.sg[3])) * decay(he, le, 0.f, 0.f);
+      dl += lane_from(wave_incl_scan_dpp(lane_from(srow, 63 - lane)), 63 - lane);          // over r >= t
+      dl += before_lane(step * gcol, lane) + s.fd[r];                                      // over i < t
+#pragma unroll
+      for (int b = 1; b < 4; ++b) {
+        const float c = before_lane(r < 16 * b ? s.cs[b - 1][r] : 0.f, lane);
+        dl += r < 16 * b ? c : 0.f;
       }
+      float raw = s.mcol[r] + s.diag[r] + gcol + A * dl;
+      const bool in = r < rows;
+      if (a.softplus) raw *= -expm1f(-step);             // sigmoid of the raw step, from its softplus
+      if (in) a.ddt[(t0 + r) * a.H + h] = raw;
+      float sa = in ? step * dl : 0.f, sd = in ? s.err[r] : 0.f, sb = in ? raw : 0.f;
+      sa = groups_sum(sum16(sa));
+      sd = groups_sum(sum16(sd));
+      sb = groups_sum(sum16(sb));
+      if (lane == 0) *(f4*)(a.sums + (slot * a.H + h) * 4) = f4{sa, sd, sb, 0.f};
+    }
     __syncthreads();
   }
+  __syncthreads();
+  __syncthreads();
+  half(dbn);
+  __syncthreads();
+  write(dbt, a.dB, a.partB);
 }
 
 // dB and dC from the shares of the splits, in order.
@@ -461,7 +531,7 @@ template <typename E, int NP>
 hipError_t chunks(const ScanArgs& a, hipStream_t st) {
   const long items = a.q.slots(C) * a.G * a.splits;
   if (items == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_ssm_bwd<E, NP>), dim3(xcd_grid(items)), dim3(NTHREADS), 0, st, a, items);
+  hipLaunchKernelGGL((k_ssm_bwd<E, NP>), dim3(xcd_grid(items)), dim3(2 * NTHREADS), 0, st, a, items);
   return hipGetLastError();
 }
 
@@ -476,8 +546,8 @@ int scan_splits(const Seqs& q, int H, int G) {
 }
 
 hipError_t launch_scan_bwd(const ScanArgs& a, int dtype, hipStream_t st) {
-  hipError_t e = hipSuccess;
-  if (a.seg) {
+  hipError_t e = launch_scan_gates(a, st);
+  if (e == hipSuccess && a.seg) {
     e = launch_scan_walks(a, dtype, 3, false, st);
     if (e == hipSuccess) e = launch_scan_compose(a, 3, st);
   }

@@ -25,21 +25,67 @@ namespace qd {
 
 namespace {
 
-// Zero-filled operand rows outside the matrices make every product exact.
+// Gates of a chunk slot's 16 heads a workgroup: the raw steps are read along
+// the heads, transposed in LDS, then a token is a lane.
+__global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
+  __shared__ float raw[16][C + 1];
+  const int hb = (a.H + 15) / 16, h0 = (int)(blockIdx.x % hb) * 16, t = threadIdx.x, lane = t & 63, w = wave_id(t);
+  const long slot = blockIdx.x / hb;
+  int n, len, pos;
+  long s0;
+  if (!a.q.locate(slot, C, n, s0, len, pos)) return;
+  const int rows = min(C, len - pos), heads = min(16, a.H - h0);
+  for (int i = t; i < 16 * C; i += NTHREADS) {
+    const int r = i >> 4, h = i & 15;
+    if (r < rows && h < heads) raw[h][r] = a.dt[(s0 + pos + r) * a.H + h0 + h];
+  }
+  __syncthreads();
+  for (int k = w; k < heads; k += NWAVES) {
+    const int h = h0 + k;
+    const float dt = lane < rows ? step_size(raw[k][lane] + (a.bias ? a.bias[h] : 0.f), a.softplus) : 0.f;
+    const double b = wave_incl_scan64((double)dt * (double)a.A[h]);
+    float* g = a.gates + (slot * a.H + h) * GATES + lane;
+    g[0] = dt;
+    g[C] = (float)b;
+    g[2 * C] = (float)(b - (double)(float)b);
+  }
+}
+
+// Whether any of a piece's values is infinite or NaN: all ones in the exponent.
+template <typename E>
+__device__ inline bool not_finite(u32x4 v) {
+  constexpr uint32_t exps = sizeof(E) == 2 ? 0x7f807f80u : 0x7f800000u, one = sizeof(E) == 2 ? 0x00800080u : 0x00800000u;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) any |= (v[i] & exps) + one;
+  return (any & (sizeof(E) == 2 ? 0x80008000u : 0x80000000u)) != 0;
+}
+
+// Operands of a chunk in LDS; rows and columns outside the matrices are zeros.
 template <typename E, int NP>
-struct FwdLds {
+struct OutLds {
   static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDC = lds_ld<E>(C), PL = sizeof(E) == 2 ? 2 : 1;
-  E B[C * LDN], Cm[C * LDN], X[C * LDP];
-  E W[PL][C * LDC];
-  Gates g;
+  struct Buf {
+    E B[C * LDN], Cm[C * LDN], X[C * LDP];
+    E W[PL][C * LDC];                  // W o C B^T diag(dt), [r][i], planes
+    Gates g;
+  };
+  static constexpr int NBUF = 2 * sizeof(Buf) + 64 <= 163840 ? 2 : 1;
+  Buf buf[NBUF];
+  int bad[2];                          // chunk + 1 whose x has an infinity or a NaN
 };
 
+// Waves 4 to 7 produce: they load the next chunk's operands into LDS and form
+// its W o C B^T diag(dt) (wave 4 + w: tokens 16 w .. of it), which needs no
+// state; waves 0 to 3 consume: outputs, then the state.  Per chunk two
+// barriers, after the operands are in LDS and at the end.  fp32 with N > 64
+// has room for one chunk in LDS only: there the two halves take turns.
 template <typename E, int NP>
-__global__ __launch_bounds__(NTHREADS, sizeof(E) == 2 ? 2 : 1) void k_ssm_out(ScanArgs a, long items) {
-  typedef FwdLds<E, NP> L;
+__global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long items) {
+  typedef OutLds<E, NP> L;
   typedef typename Q4<E>::t q4;
   __shared__ __attribute__((aligned(16))) L s;
-  constexpr int NB = NP / 16, KN = NP / 32, PL = L::PL;
+  constexpr int NB = NP / 16, KN = NP / 32, PL = L::PL, NBUF = L::NBUF;
   long item;
   if (!xcd_item(items, item)) return;
   const int pts = p_tiles(a.P), hp = (int)(item % (a.H * pts)), h = hp / pts, p0 = hp % pts * PT;
@@ -54,17 +100,90 @@ __global__ __launch_bounds__(NTHREADS, sizeof(E) == 2 ? 2 : 1) void k_ssm_out(Sc
   } else if (!a.q.locate(slot, a.seg, n, s0, len, pos)) {
     return;
   }
-  const int end = whole ? len : min(pos + a.seg, len);
-  const int t = threadIdx.x, lane = t & 63, w = wave_id(t), g4 = 4 * (lane >> 4), col = lane & 15;
+  const int end = whole ? len : min(pos + a.seg, len), chunks = (end - pos + C - 1) / C;
+  const int t = threadIdx.x & (NTHREADS - 1), lane = t & 63, wave = wave_id(threadIdx.x), w = wave & 3;
+  const int g4 = 4 * (lane >> 4), col = lane & 15;
   const int cols = min(PT, a.P - p0), grp = h / (a.H / a.G);
-  const E* x = (const E*)a.x + (s0 + pos) * a.ldx + (long)h * a.P + p0;
-  const E* B = (const E*)a.B + (s0 + pos) * a.ldb + (long)grp * a.N;
-  const E* Cm = (const E*)a.C + (s0 + pos) * a.ldc + (long)grp * a.N;
-  const bool vx = vec_rows<E>(x, a.ldx, cols), vb = vec_rows<E>(B, a.ldb, a.N), vc = vec_rows<E>(Cm, a.ldc, a.N);
+
+  if (wave >= 4) {
+    const E* x = (const E*)a.x + (s0 + pos) * a.ldx + (long)h * a.P + p0;
+    const E* B = (const E*)a.B + (s0 + pos) * a.ldb + (long)grp * a.N;
+    const E* Cm = (const E*)a.C + (s0 + pos) * a.ldc + (long)grp * a.N;
+    const bool vx = vec_rows<E>(x, a.ldx, cols), vb = vec_rows<E>(B, a.ldb, a.N), vc = vec_rows<E>(Cm, a.ldc, a.N);
+    const long cslot = (a.q.cu ? s0 / C + n : (long)n * ((a.q.T + C - 1) / C)) + pos / C;
+    Stage<E, PT, NTHREADS> rx;
+    Stage<E, NP, NTHREADS> rb, rc;
+    float rg = 0.f;
+    auto fetch = [&](int c) {
+      const int rows = min(C, end - pos - c * C);
+      rx.load(x + (long)c * C * a.ldx, a.ldx, rows, cols, vx, t);
+      rb.load(B + (long)c * C * a.ldb, a.ldb, rows, a.N, vb, t);
+      rc.load(Cm + (long)c * C * a.ldc, a.ldc, rows, a.N, vc, t);
+      if (t < GATES) rg = a.gates[((cslot + c) * a.H + h) * GATES + t];
+    };
+    auto put = [&](int c) {
+      typename L::Buf& u = s.buf[c % NBUF];
+      rx.put(u.X, L::LDP, t);
+      rb.put(u.B, L::LDN, t);
+      rc.put(u.Cm, L::LDN, t);
+      if (t < GATES) ((float*)&u.g)[t] = rg;
+      bool bad = false;
+#pragma unroll
+      for (int k = 0; k < rx.K; ++k) bad |= not_finite<E>(rx.r[k]);
+      if (bad) s.bad[c & 1] = c + 1;
+    };
+    // rows r = 16 w + col, formed as their transposes: accumulator rows are i
+    auto scores = [&](int c) {
+      typename L::Buf& u = s.buf[c % NBUF];
+      Fr<E> cf[KN];
+#pragma unroll
+      for (int k = 0; k < KN; ++k) cf[k] = row_frag<E>(u.Cm, L::LDN, 16 * w, 32 * k, lane);
+      const int r = 16 * w + col;
+      const float hr = u.g.bh[r], lr = u.g.bl[r];
+#pragma unroll
+      for (int ib = 0; ib < 4; ++ib) {
+        if (ib > (w | 1)) break;         // products take blocks in pairs: the one beside the last is zero
+        f4 v = zero4();
+        if (ib <= w) {
+#pragma unroll
+          for (int k = 0; k < KN; ++k) v = mma(row_frag<E>(u.B, L::LDN, 16 * ib, 32 * k, lane), cf[k], v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 16 * ib + g4 + j;
+            v[j] = i <= r ? v[j] * decay(hr, lr, u.g.bh[i], u.g.bl[i]) * u.g.dt[i] : 0.f;
+          }
+        }
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) {
+          const q4 q = narrow<E>(v);
+          *(q4*)(u.W[pl] + r * L::LDC + 16 * ib + g4) = q;
+          if (pl + 1 < PL) v -= widen<E>(q);
+        }
+      }
+    };
+    if (t < 2) s.bad[t] = 0;
+    if (chunks > 0) fetch(0);
+    __syncthreads();
+    if (chunks > 0) put(0);
+    if (chunks > 1) fetch(1);
+    __syncthreads();
+    if (chunks > 0) scores(0);
+    __syncthreads();
+    for (int c = 0; c < chunks; ++c) {
+      if (NBUF == 1) __syncthreads();    // the consumers have read this chunk
+      const bool more = c + 1 < chunks;
+      if (more) put(c + 1);
+      __syncthreads();
+      if (c + 2 < chunks) fetch(c + 2);
+      if (more) scores(c + 1);
+      __syncthreads();
+    }
+    return;
+  }
+
   E* y = (E*)a.y + ((s0 + pos) * a.H + h) * (long)a.P + p0;
   const bool vy = a.P % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(E) - 1)) == 0;
   const float D = a.D ? a.D[h] : 0.f;
-
   // state: f4 S[nb] holds n = 16 nb + g4 + j of row p = p0 + 16 w + col
   const int p = p0 + 16 * w + col;
   const float* in = whole ? (a.S0 ? a.S0 + ((long)n * a.H + h) * a.P * a.N : nullptr)
@@ -77,106 +196,96 @@ __global__ __launch_bounds__(NTHREADS, sizeof(E) == 2 ? 2 : 1) void k_ssm_out(Sc
       const int nn = 16 * nb + g4 + j;
       S[nb][j] = in && p < a.P && nn < a.N ? in[(long)p * a.N + nn] : 0.f;
     }
-
-  Stage<E, PT, NTHREADS> rx;
-  Stage<E, NP, NTHREADS> rb, rc;
-  auto fetch = [&](int at) {
-    const int rows = min(C, end - at), d = at - pos;
-    rx.load(x + d * a.ldx, a.ldx, rows, cols, vx, t);
-    rb.load(B + d * a.ldb, a.ldb, rows, a.N, vb, t);
-    rc.load(Cm + d * a.ldc, a.ldc, rows, a.N, vc, t);
-  };
-  if (pos < end) fetch(pos);
-  for (int at = pos; at < end; at += C) {
-    const int rows = min(C, end - at);
-    rx.put(s.X, L::LDP, t);
-    rb.put(s.B, L::LDN, t);
-    rc.put(s.Cm, L::LDN, t);
-    if (w == 0) chunk_gates(s.g, a, s0 + at, rows, h, lane);
-    __syncthreads();
-    if (at + C < end) fetch(at + C);
-
-    // rows r = 16 w + col of W o C B^T diag(dt), as their transposes: accumulator rows are i
-    {
-      Fr<E> c[KN];
+  __syncthreads();
+  __syncthreads();
+  __syncthreads();
+  for (int c = 0; c < chunks; ++c) {
+    const typename L::Buf& u = s.buf[c % NBUF];
+    const int rows = min(C, end - pos - c * C);
+    Fr<E> xt[2];                         // x^T: row p, k = i
 #pragma unroll
-      for (int k = 0; k < KN; ++k) c[k] = row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane);
-      const int r = 16 * w + col;
-      const float hr = s.g.bh[r], lr = s.g.bl[r];
+    for (int k = 0; k < 2; ++k) xt[k] = col_frag<E>(u.X, L::LDP, 32 * k, 16 * w, lane);
+    // An infinity or a NaN in x must not meet the zero weights of the tokens
+    // before it: it is taken out, and what it enters becomes NaN.
+    int first = C;                       // token of row p's first one
+    if (s.bad[c & 1] == c + 1) {
 #pragma unroll
-      for (int ib = 0; ib < 4; ++ib) {
-        if (ib > (w | 1)) break;       // products take blocks in pairs: the one beside the last is zero
-        f4 v = zero4();
-        if (ib <= w) {
+      for (int k = 0; k < 2; ++k) {
+        f4 v[2];
+        quads<E>(xt[k], v[0], v[1]);
 #pragma unroll
-          for (int k = 0; k < KN; ++k) v = mma(row_frag<E>(s.B, L::LDN, 16 * ib, 32 * k, lane), c[k], v);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 16 * ib + g4 + j;
-            v[j] = i <= r ? v[j] * decay(hr, lr, s.g.bh[i], s.g.bl[i]) * s.g.dt[i] : 0.f;
+        for (int i = 0; i < 8; ++i) {
+          const bool fine = fabsf(v[i / 4][i % 4]) < __builtin_inff();
+          if (!fine) {
+            first = min(first, 32 * k + 16 * (i / 4) + g4 + i % 4);
+            v[i / 4][i % 4] = 0.f;
           }
         }
-#pragma unroll
-        for (int pl = 0; pl < PL; ++pl) {
-          const q4 q = narrow<E>(v);
-          *(q4*)(s.W[pl] + r * L::LDC + 16 * ib + g4) = q;
-          if (pl + 1 < PL) v -= widen<E>(q);
-        }
+        xt[k] = planes<E, 1>(v[0], v[1]).p[0];
       }
+      first = min(first, __shfl_xor(first, 16, 64));
+      first = min(first, __shfl_xor(first, 32, 64));
     }
-    // Y^T rows p, columns r: from the entry state
+    // Y^T: rows p, columns r
     f4 o[4];
 #pragma unroll
-    for (int rb4 = 0; rb4 < 4; ++rb4) o[rb4] = zero4();
+    for (int b = 0; b < 4; ++b) o[b] = zero4();
 #pragma unroll
     for (int k = 0; k < KN; ++k) {
       const Planes<E, 2> sp = planes<E, 2>(S[2 * k], S[2 * k + 1]);
 #pragma unroll
-      for (int rb4 = 0; rb4 < 4; ++rb4) o[rb4] = mma(sp, row_frag<E>(s.Cm, L::LDN, 16 * rb4, 32 * k, lane), o[rb4]);
+      for (int b = 0; b < 4; ++b) o[b] = mma(sp, row_frag<E>(u.Cm, L::LDN, 16 * b, 32 * k, lane), o[b]);
     }
-    Fr<E> xt[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) xt[k] = col_frag<E>(s.X, L::LDP, 32 * k, 16 * w, lane);
-    __syncthreads();
+    for (int b = 0; b < 4; ++b) {
+      const int r = 16 * b + col;
+      o[b] *= decay(u.g.bh[r], u.g.bl[r], 0.f, 0.f);
 #pragma unroll
-    for (int rb4 = 0; rb4 < 4; ++rb4) {
-      const int r = 16 * rb4 + col;
-      o[rb4] *= decay(s.g.bh[r], s.g.bl[r], 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k <= rb4 / 2; ++k)
+      for (int k = 0; k <= b / 2; ++k)
 #pragma unroll
         for (int pl = PL - 1; pl >= 0; --pl)
-          o[rb4] = mma(xt[k], row_frag<E>(s.W[pl], L::LDC, 16 * rb4, 32 * k, lane), o[rb4]);
-      if (a.D) o[rb4] += D * widen<E>(*(const q4*)(s.X + r * L::LDP + 16 * w + g4));
+          o[b] = mma(xt[k], row_frag<E>(u.W[pl], L::LDC, 16 * b, 32 * k, lane), o[b]);
+      if (a.D) o[b] += D * widen<E>(*(const q4*)(u.X + r * L::LDP + 16 * w + g4));
+      if (s.bad[c & 1] == c + 1)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (r >= __shfl(first, g4 + j, 64)) o[b][j] = __builtin_nanf("");
       if (r < rows) {
         const int pc = 16 * w + g4;
-        E* out = y + (long)(at - pos + r) * a.H * a.P + pc;
+        E* out = y + (long)(c * C + r) * a.H * a.P + pc;
         if (vy) {
-          if (pc < cols) *(q4*)out = narrow<E>(o[rb4]);
+          if (pc < cols) *(q4*)out = narrow<E>(o[b]);
         } else {
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (pc + j < cols) out[j] = fromf<E>(o[rb4][j]);
+            if (pc + j < cols) out[j] = fromf<E>(o[b][j]);
         }
       }
     }
-    // S' : accumulator rows n, columns p
-    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
+    if (NBUF == 2) __syncthreads();
+    // S': rows n, columns p
+    const float he = u.g.bh[C - 1], le = u.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) S[nb] *= total;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      f4 u, v;
-      quads<E>(xt[k], u, v);
+      f4 v[2];
+      quads<E>(xt[k], v[0], v[1]);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 32 * k + g4 + j;
-        u[j] *= s.g.dt[i] * decay(he, le, s.g.bh[i], s.g.bl[i]);
-        v[j] *= s.g.dt[i + 16] * decay(he, le, s.g.bh[i + 16], s.g.bl[i + 16]);
+      for (int i = 0; i < 8; ++i) {
+        const int r = 32 * k + 16 * (i / 4) + g4 + i % 4;
+        v[i / 4][i % 4] *= u.g.dt[r] * decay(he, le, u.g.bh[r], u.g.bl[r]);
       }
-      const Planes<E, 3> xw = planes<E, 3>(u, v);
+      const Planes<E, 3> xw = planes<E, 3>(v[0], v[1]);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane), xw, S[nb]);
+      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(col_frag<E>(u.B, L::LDN, 32 * k, 16 * nb, lane), xw, S[nb]);
+    }
+    if (first < C)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) S[nb] = zero4() + __builtin_nanf("");
+    if (NBUF == 1) {
+      __syncthreads();
+      __syncthreads();
     }
     __syncthreads();
   }
@@ -249,14 +358,16 @@ __global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items
 
   Stage<E, PT, NTHREADS> rx;
   Stage<E, NP, NTHREADS> rb;
+  float rg = 0.f;
   auto fetch = [&](int c) {
     const int rows = min(C, end - pos - c * C);
     rx.load(x + (long)c * C * ldx, ldx, rows, cols, vx, t);
     rb.load(B + (long)c * C * ldb, ldb, rows, a.N, vb, t);
+    if (t < GATES) rg = a.gates[((cslot + c) * a.H + h) * GATES + t];
   };
   if (chunks > 0) fetch(dir ? chunks - 1 : 0);
   for (int k0 = 0; k0 < chunks; ++k0) {
-    const int c = dir ? chunks - 1 - k0 : k0, rows = min(C, end - pos - c * C);
+    const int c = dir ? chunks - 1 - k0 : k0;
     if (keep) {
       float* out = (dir ? a.grads : a.states) + ((cslot + c) * a.H * pts + hp) * (long)(PT * NP);
 #pragma unroll
@@ -264,7 +375,7 @@ __global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items
     }
     rx.put(s.X, L::LDP, t);
     rb.put(s.B, L::LDN, t);
-    if (w == 0) chunk_gates(s.g, a, s0 + pos + c * C, rows, h, lane);
+    if (t < GATES) ((float*)&s.g)[t] = rg;
     __syncthreads();
     if (k0 + 1 < chunks) fetch(dir ? c - 1 : c + 1);
     const float he = s.g.bh[C - 1], le = s.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
@@ -376,7 +487,7 @@ template <typename E, int NP>
 hipError_t out_walk(const ScanArgs& a, hipStream_t st) {
   const long items = walk_slots(a) * a.H * p_tiles(a.P);
   if (items == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_ssm_out<E, NP>), dim3(xcd_grid(items)), dim3(NTHREADS), 0, st, a, items);
+  hipLaunchKernelGGL((k_ssm_out<E, NP>), dim3(xcd_grid(items)), dim3(2 * NTHREADS), 0, st, a, items);
   return hipGetLastError();
 }
 
@@ -417,9 +528,18 @@ int scan_segment(const Seqs& q, int H, int P, int dirs) {
   return q.T <= chunks * C ? 0 : (int)(chunks * C);
 }
 
+hipError_t launch_scan_gates(const ScanArgs& a, hipStream_t st) {
+  const long blocks = a.q.slots(C) * ((a.H + 15) / 16);
+  if (blocks == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_ssm_gates, dim3((unsigned)blocks), dim3(NTHREADS), 0, st, a);
+  return hipGetLastError();
+}
+
 hipError_t launch_scan_fwd(const ScanArgs& a, int dtype, hipStream_t st) {
+  hipError_t e = launch_scan_gates(a, st);
+  if (e != hipSuccess) return e;
   if (a.seg) {
-    hipError_t e = launch_scan_walks(a, dtype, 1, false, st);
+    e = launch_scan_walks(a, dtype, 1, false, st);
     if (e == hipSuccess) e = launch_scan_compose(a, 1, st);
     if (e != hipSuccess) return e;
   }

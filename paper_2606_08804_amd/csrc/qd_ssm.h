@@ -39,15 +39,34 @@ template <typename E, int PL> struct Planes {
   static constexpr int N = sizeof(E) == 2 ? PL : 1;
   Fr<E> p[N];
 };
+// Two fp32 values as bf16 in one register (one instruction: without the line
+// that hides where the register comes from, taking the values apart again makes
+// the compiler convert each by itself and join them).
+__device__ inline uint32_t pack2(float x, float y) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  uint32_t r = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x, y}, b2));
+  asm("" : "+v"(r));
+  return r;
+}
+// A quad as bf16; plane4 also leaves in v what that rounds off.
+__device__ inline uint2 pack4(const f4& v) { return make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3])); }
+__device__ inline uint2 plane4(f4& v) {
+  const uint2 r = pack4(v);
+  v[0] -= __builtin_bit_cast(float, r.x << 16);
+  v[1] -= __builtin_bit_cast(float, r.x & 0xffff0000u);
+  v[2] -= __builtin_bit_cast(float, r.y << 16);
+  v[3] -= __builtin_bit_cast(float, r.y & 0xffff0000u);
+  return r;
+}
 template <typename E, int PL>
 __device__ inline Planes<E, PL> planes(f4 x, f4 y) {
   Planes<E, PL> r;
   if constexpr (sizeof(E) == 2) {
-    f8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      r.p[i].v = __builtin_convertvector(v, bf8);
-      if (i + 1 < PL) v -= __builtin_convertvector(r.p[i].v, f8);
+      const uint2 p = i + 1 < PL ? plane4(x) : pack4(x), q = i + 1 < PL ? plane4(y) : pack4(y);
+      r.p[i].v = __builtin_bit_cast(bf8, u32x4{p.x, p.y, q.x, q.y});
     }
   } else {
     r.p[0].a = x;
@@ -83,23 +102,64 @@ __device__ inline typename Q4<E>::t narrow(f4 q) {
   else return q;
 }
 
-// LDS row length in elements: 16 bytes of padding spread rows over the banks.
-template <typename E> constexpr int lds_ld(int cols) { return cols + 16 / (int)sizeof(E); }
+// A quad's planes one after the other to p, p + step (fp32: the quad itself).
+template <typename E, int PL>
+__device__ inline void put_planes(E* p, int step, f4 x) {
+#pragma unroll
+  for (int i = 0; i < PL; ++i) {
+    if constexpr (sizeof(E) == 2) {
+      *(uint2*)(p + i * step) = i + 1 < PL ? plane4(x) : pack4(x);
+    } else {
+      *(f4*)p = x;
+    }
+  }
+}
+
+// LDS tiles are row-major, rows `lds_ld` elements apart.  In bf16 tiles the two
+// 16-byte halves of every 16 columns change places in rows 8 to 15 of 16
+// (`flip`): rows then lie 8 banks apart, and the three ways they are accessed
+// (16-byte pieces of a row, quads of 16 rows at one column, transpose reads of
+// four rows by 16 columns) each meet every bank once.
+template <typename E> constexpr int lds_ld(int cols) { return cols + (sizeof(E) == 2 ? 16 : 4); }
+template <typename E> __device__ inline int flip(int row, int c) { return sizeof(E) == 2 ? c ^ (row & 8) : c; }
+
+// Tiles that are read along rows alone ("steps") hold a row's columns in groups
+// of 32 in the order in which a step takes them, the quad 16 blk + 4 g of a group
+// at 8 g + 4 blk: a lane's two quads are then one 16-byte read.  (Two 8-byte
+// reads are joined into one instruction, which takes 16 lanes at a time and so
+// meets half of the banks twice; transpose reads of this order would.)
+template <typename E> constexpr int steps_ld(int cols) { return cols + 16 / (int)sizeof(E); }
+template <typename E> __device__ constexpr int step_at(int c) {
+  return sizeof(E) == 2 ? (c & ~31) + ((c >> 2) & 3) * 8 + ((c >> 4) & 1) * 4 : c;
+}
+template <typename E>
+__device__ inline Fr<E> step_frag(const E* t, int ld, int row0, int k0, int lane) {
+  Fr<E> f;
+  if constexpr (sizeof(E) == 2) {
+    f.v = *(const bf8*)(t + (row0 + (lane & 15)) * ld + k0 + 8 * (lane >> 4));
+  } else {
+    const E* p = t + (row0 + (lane & 15)) * ld + k0 + 4 * (lane >> 4);
+    f.a = *(const f4*)p;
+    f.b = *(const f4*)(p + 16);
+  }
+  return f;
+}
 
 // Operand with i = row0 + l % 16 and k along the row, from k0.
 template <typename E>
 __device__ inline Fr<E> row_frag(const E* t, int ld, int row0, int k0, int lane) {
   typedef typename Q4<E>::t q4;
-  const E* p = t + (row0 + (lane & 15)) * ld + k0 + 4 * (lane >> 4);
+  const int r = lane & 15;
+  const E* p = t + (row0 + r) * ld + k0 + flip<E>(r, 4 * (lane >> 4));
   const q4 a = *(const q4*)p, b = *(const q4*)(p + 16);
-  Fr<E> r;
+  Fr<E> f;
   if constexpr (sizeof(E) == 2) {
-    r.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    f.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
   } else {
-    r.a = a;
-    r.b = b;
+    f.a = a;
+    f.b = b;
   }
-  return r;
+  return f;
 }
 // Operand with i = column j0 + l % 16 and k down the rows, from row k0: the LDS
 // transpose read for bf16 (a group of 16 lanes names the 8-byte pieces of a 4 x
@@ -109,8 +169,8 @@ __device__ inline Fr<E> col_frag(const E* t, int ld, int k0, int j0, int lane) {
   Fr<E> r;
   if constexpr (sizeof(E) == 2) {
     typedef __attribute__((address_space(3))) bf4* lp;
-    const int L = lane & 15;
-    const E* p = t + (k0 + 4 * (lane >> 4) + (L >> 2)) * ld + j0 + 4 * (L & 3);
+    const int L = lane & 15, row = 4 * (lane >> 4) + (L >> 2);
+    const E* p = t + (k0 + row) * ld + j0 + flip<E>(row, 4 * (L & 3));
     const bf4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lp)(uintptr_t)(uint32_t)(uintptr_t)p);
     const bf4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lp)(uintptr_t)(uint32_t)(uintptr_t)(p + 16 * ld));
     r.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
@@ -178,44 +238,98 @@ __device__ inline bool xcd_item(long n, long& item) {
 }
 inline unsigned xcd_grid(long n) { return (unsigned)((n + 7) / 8 * 8); }
 
+// Two waves a SIMD are what these kernels' LDS allows: their registers are theirs to use.
+#define QD_TWO_WAVES __attribute__((amdgpu_waves_per_eu(2, 2)))
+// A line that the scheduler moves nothing across.  Operands are read in batches
+// before it and multiplied after it: left alone, the compiler reads each right
+// before its product, which then waits out the LDS's latency.
+__device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
+
+// The lane number as a value the compiler cannot trace: what is formed from it
+// (LDS addresses, masks of the triangles) is formed again every turn of a
+// loop instead of being kept in registers, which are all taken (hoisted, 130
+// such values went to scratch memory and back).
+__device__ inline int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // A tile of 64 rows x COLS staged through registers: loads first, LDS later.
-// Rows from `rows` and columns from `cols` on are zeros.
+// Rows from `rows` and columns from `cols` on are zeros: a row past the last
+// lies past the end of the buffer that the load names, which reads as zero, and
+// so do the lanes of columns past the last.  A load then is one instruction, with
+// a lane offset formed once (as masked 64-bit addresses the ten loads of a
+// chunk took their wave 2500 cycles).
+__device__ inline __amdgpu_buffer_rsrc_t buffer(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+// Four consecutive values per lane to a tile of rows: lanes whose offset lies
+// past the buffer's end (rows past the last, by the buffer's size; columns past
+// the last, by an offset of 2^31) write nothing.
+template <typename E>
+__device__ inline void store_quad(__amdgpu_buffer_rsrc_t b, uint32_t off, f4 v) {
+  if constexpr (sizeof(E) == 2) {
+    typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, narrow<E>(v)), b, off, 0, 0);
+  } else {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), b, off, 0, 0);
+  }
+}
 template <typename E, int COLS, int NT>
 struct Stage {
-  static constexpr int V = 16 / (int)sizeof(E), PIECES = 64 * COLS / V, K = PIECES / NT;
-  static_assert(PIECES % NT == 0, "pieces split evenly");
+  static constexpr int V = 16 / (int)sizeof(E), PIECES = 64 * COLS / V, K = PIECES / NT, STEP = NT / (COLS / V);
+  static_assert(PIECES % NT == 0 && NT % (COLS / V) == 0, "pieces split evenly, by whole rows");
   u32x4 r[K];
-  __device__ inline void load(const E* src, long ld, int rows, int cols, bool vec, int t) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int i = k * NT + t, row = i / (COLS / V), c = i % (COLS / V) * V;
-      r[k] = u32x4{0, 0, 0, 0};
-      if (row >= rows || c >= cols) continue;
-      const E* p = src + row * ld + c;
-      if (vec) {
-        r[k] = *(const u32x4*)p;
-      } else {
-        E e[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) e[j] = c + j < cols ? p[j] : fromf<E>(0.f);
-        r[k] = __builtin_bit_cast(u32x4, e);
-      }
-    }
+  // Byte offset of a thread's first piece, and from one of its pieces to the next.
+  static __device__ inline uint32_t offset(long ld, int cols, int t) {
+    const int c = t % (COLS / V) * V;
+    return c < cols ? (uint32_t)((t / (COLS / V)) * ld + c) * (uint32_t)sizeof(E) : 0x80000000u;
   }
-  __device__ inline void put(E* dst, int ld, int t) const {
+  // Nothing is loaded where rows are not whole pieces: `put` then copies them.
+  __device__ inline void load(const E* src, long ld, int rows, bool vec, uint32_t off) {
+    const __amdgpu_buffer_rsrc_t b = buffer(uniform_ptr(src), vec ? (uint32_t)(rows * ld) * (uint32_t)sizeof(E) : 0u);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int i = k * NT + t, row = i / (COLS / V), c = i % (COLS / V) * V;
-      *(u32x4*)(dst + row * ld + c) = r[k];
+    for (int k = 0; k < K; ++k)
+      r[k] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(b, off + (uint32_t)(k * STEP * ld) * (uint32_t)sizeof(E), 0, 0));
+  }
+  // src, ld, rows and cols as of the load.
+  template <bool STEPS = false>
+  __device__ inline void put(E* dst, int ldd, const E* src, long ld, int rows, int cols, bool vec, int t) const {
+    if (vec) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int row = t / (COLS / V) + k * STEP, c = t % (COLS / V) * V;
+        if constexpr (STEPS && sizeof(E) == 2) {   // two quads of one block
+          typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+          E* d = dst + row * ldd + step_at<E>(c);
+          *(u32x2*)d = u32x2{r[k][0], r[k][1]};
+          *(u32x2*)(d + 8) = u32x2{r[k][2], r[k][3]};
+        } else {
+          *(u32x4*)(dst + row * ldd + flip<E>(row, c)) = r[k];
+        }
+      }
+    } else {
+      for (int i = t; i < 64 * COLS; i += NT) {
+        const int row = i / COLS, c = i % COLS;
+        dst[row * ldd + (STEPS ? step_at<E>(c & ~3) + (c & 3) : flip<E>(row, c))] =
+            row < rows && c < cols ? src[row * ld + c] : fromf<E>(0.f);
+      }
     }
   }
 };
 
-// Whether rows of `cols` values, `ld` apart from p on, are whole aligned 16-byte pieces.
+// Whether quads of rows of `cols` values, `ld` apart, are whole and aligned
+// (and 64 rows lie within a store's offsets).
+template <typename E>
+__device__ inline bool quad_rows(const void* p, long ld, int cols) {
+  return ((uintptr_t)p & (4 * sizeof(E) - 1)) == 0 && ld % 4 == 0 && cols % 4 == 0 && ld < (1L << 24) / (int)sizeof(E);
+}
+// Whether rows of `cols` values, `ld` apart from p on, are whole aligned
+// 16-byte pieces (and 64 of them lie within a load's offsets).
 template <typename E>
 __device__ inline bool vec_rows(const void* p, long ld, int cols) {
   constexpr int V = 16 / (int)sizeof(E);
-  return ((uintptr_t)p & 15) == 0 && ld % V == 0 && cols % V == 0;
+  return ((uintptr_t)p & 15) == 0 && ld % V == 0 && cols % V == 0 && ld < (1L << 24) / (int)sizeof(E);
 }
 
 template <int CTRL, int ROWS, bool BOUND>
@@ -241,14 +355,28 @@ __device__ inline double wave_incl_scan64(double x) {
 // would leave a single float's differences after it off by 6e-4.  Tokens past
 // the chunk's end have dt = 0, so that b stays where it is.
 struct Gates {
-  float dt[C], bh[C], bl[C];
+  float dt[C], bh[C], bl[C];         // dt, b
+  float head[C], tail[C];            // e^{b_r}, e^{b_C - b_i}
+  float head16[C], tail16[C];        // the same from the end of the 16 tokens before and to the end of its own 16
 };
-constexpr int GATES = 3 * C;
+constexpr int GATES = 7 * C;
+// One of the values of a chunk's gates (threads past them get zero).
+__device__ inline float load_gate(const float* gates, int t) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(uniform_ptr(gates)), 0, GATES * 4, 0x00020000), 4 * t, 0, 0));
+}
 __device__ inline float step_size(float z, int softplus) {
   return softplus ? fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) : z;
 }
-// exp(b_r - b_i); exp(b_r) with zeros for b_i.
+// exp(b_r - b_i).
 __device__ inline float decay(float hr, float lr, float hi, float li) { return fast_exp((hr - hi) + (lr - li)); }
+
+// exp of b's step from the end of block i to the end of the block before r's
+// (i < r, blocks of 16): what head16 and tail16 leave out of exp(b_r - b_i).
+__device__ inline float between(const Gates& g, int r, int i) {
+  const int e = 16 * r - 1, f = 16 * i + 15;
+  return decay(g.bh[e], g.bl[e], g.bh[f], g.bl[f]);
+}
 
 hipError_t launch_scan_gates(const ScanArgs& a, hipStream_t st);
 hipError_t launch_scan_fwd(const ScanArgs& a, int dtype, hipStream_t st);

@@ -20,12 +20,14 @@
 // then chunks are independent.  A workgroup takes a chunk and loops over the
 // heads of a group (or a share of them: `splits`, whose dB and dC are then
 // summed in order), with K and the group's dB and dC in registers.  Waves 0 to
-// 3 form dC (S, E^T) and G B^T, waves 4 to 7 dB and dX (G, E); of each four
+// 3 form dC (S, E^T) and G B^T, waves 4 to 7 dB and dx (G, E); of each four
 //   wave w, tokens 16 w ..      the products over the chunk's tokens, from
 //                               E and E^T as they stand in the accumulators;
 //   wave w, a quarter of n      the products with S and G, whose operands are
 //                               read straight from the walks' register order;
 //   wave w, rows 16 w .. of p   G B^T, with G through LDS.
+// A spilled register costs more than its own bytes: its reload waits for every
+// prefetch issued before it.
 #include "qd_ssm.h"
 
 namespace qd {
@@ -34,31 +36,22 @@ namespace {
 
 template <typename E, int NP>
 struct BwdLds {
-  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), PL = sizeof(E) == 2 ? 2 : 1;
-  static constexpr int LDS_ = lds_ld<float>(NP), LDT = lds_ld<float>(PT);
-  E B[C * LDN], Cm[C * LDN], X[C * LDP], dY[C * LDP];
+  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDX = steps_ld<E>(PT), PL = sizeof(E) == 2 ? 2 : 1;
+  static constexpr int LDS_ = lds_ld<float>(NP), LDT = sizeof(E) == 4 && NP == 128 ? PT : lds_ld<float>(PT);   // (no room for padding there)
+  E B[C * LDN], Cm[C * LDN], dY[C * LDP];
+  E X[C * LDX];                      // steps
   union {
     E G[PL][NP * LDP];               // G^T: [n][p], planes
     float sum[C * LDS_];             // the end: one half of dC, of dB
   };
   float dX[C * LDT];                 // [i][p]: the part of dX with G
   Gates g;
-  float cs[3][C], fd[C];             // M: sums over r in block w > 0 by i < 16 w; pairs with r in t's own block
-  float mcol[C], diag[C], err[C], srow[4][C], gcol[4][C], sg[4];
+  struct Sums {                      // of a head, over its tiles
+    float cs[3][C], fd[C];           // M: sums over r in block w > 0 by i < 16 w; pairs with r in t's own block
+    float mcol[C], diag[C], err[C], srow[4][C], gcol[4][C], sg[4], dt[C], total;
+  };
+  Sums sums[2];                      // this head's and the one's before
 };
-
-// Keeps the scheduler from drawing the loads of one phase of a turn into the
-// phase before, where all registers are taken.
-__device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
-
-// The lane number as a value the compiler cannot trace: what is formed from it
-// (LDS addresses, masks of the triangles) is formed again every turn of the
-// loop over heads instead of being kept in registers, which are all taken
-// (hoisted, 130 such values went to scratch memory and back).
-__device__ inline int fresh(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
 
 // Sum over the four lane groups (the rows of an accumulator's columns).
 __device__ inline float groups_sum(float x) {
@@ -74,11 +67,11 @@ __device__ inline float before_lane(float x, int lane) {
 }
 
 template <typename E, int NP>
-__global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long items) {
+__global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanArgs a, long items) {
   typedef BwdLds<E, NP> L;
   typedef typename Q4<E>::t q4;
   __shared__ __attribute__((aligned(16))) L s;
-  constexpr int NB = NP / 16, KN = NP / 32, NQ = NB / 4, PL = L::PL, NT = 2 * NTHREADS;
+  constexpr int NB = NP / 16, KN = NP / 32, NQ = NB / 4, PL = L::PL, NT = NTHREADS;
   long item;
   if (!xcd_item(items, item)) return;
   const int per = a.G * a.splits, grp = (int)(item % per) / a.splits, split = (int)(item % a.splits);
@@ -86,54 +79,61 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long it
   int n, len, pos;
   long s0;
   if (!a.q.locate(slot, C, n, s0, len, pos)) return;
-  const int rows = min(C, len - pos), t = threadIdx.x, lane0 = t & 63, lane = lane0, wave = wave_id(t), w = wave & 3;
-  const int g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;     // this lane's token in the products over tokens
+  const int rows = min(C, len - pos), tid = threadIdx.x, wave = wave_id(tid), w = wave & 3;
   const long t0 = s0 + pos;
   const int pts = p_tiles(a.P), hg = a.H / a.G;
   const int h0 = grp * hg + hg * split / a.splits, h1 = grp * hg + hg * (split + 1) / a.splits;
   const int turns = (h1 - h0) * pts;
+  const long ldy = (long)a.H * a.P;
 
+  // Staging: the first half of the threads loads B, then every turn's x; the
+  // second C, then dy.  Both read rows of one matrix.
+  const int half = wave >> 2, st = tid & (NT - 1);
   {
-    Stage<E, NP, NT> rb, rc;
-    const E* B = (const E*)a.B + t0 * a.ldb + (long)grp * a.N;
-    const E* Cm = (const E*)a.C + t0 * a.ldc + (long)grp * a.N;
-    rb.load(B, a.ldb, rows, a.N, vec_rows<E>(B, a.ldb, a.N), t);
-    rc.load(Cm, a.ldc, rows, a.N, vec_rows<E>(Cm, a.ldc, a.N), t);
-    rb.put(s.B, L::LDN, t);
-    rc.put(s.Cm, L::LDN, t);
+    Stage<E, NP, NT> r;
+    const long ld = half ? a.ldc : a.ldb;
+    const E* m = (const E*)(half ? a.C : a.B) + t0 * ld + (long)grp * a.N;
+    const bool vec = vec_rows<E>(m, ld, a.N);
+    r.load(m, ld, rows, vec, r.offset(ld, a.N, st));
+    r.put(half ? s.Cm : s.B, L::LDN, m, ld, rows, a.N, vec, st);
   }
-  Stage<E, PT, NT> rx, ry;
+  Stage<E, PT, NT> rt;
   float rg = 0.f;
+  const long ldt = half ? ldy : a.ldx;
+  const E* tile0 = (half ? (const E*)a.dy : (const E*)a.x) + t0 * ldt + (long)h0 * a.P;
+  // whole pieces in one tile of a head are whole pieces in all of them
+  const bool vt = a.P % (16 / (int)sizeof(E)) == 0 && vec_rows<E>(tile0, ldt, a.P);
   auto fetch = [&](int turn) {
-    const int h = h0 + turn / pts, pt = turn % pts, cols = min(PT, a.P - pt * PT);
-    const E* x = (const E*)a.x + t0 * a.ldx + (long)h * a.P + pt * PT;
-    const E* dy = (const E*)a.dy + (t0 * a.H + h) * a.P + pt * PT;
-    rx.load(x, a.ldx, rows, cols, vec_rows<E>(x, a.ldx, cols), t);
-    ry.load(dy, (long)a.H * a.P, rows, cols, vec_rows<E>(dy, (long)a.H * a.P, cols), t);
-    if (t < GATES) rg = a.gates[(slot * a.H + h) * GATES + t];
+    const int p0 = turn % pts * PT, st = fresh(tid) & (NT - 1);
+    rt.load(tile0 + (long)(turn / pts) * a.P + p0, ldt, rows, vt, rt.offset(ldt, min(PT, a.P - p0), st));
+    rg = load_gate(a.gates + (slot * a.H + h0 + turn / pts) * GATES, tid);
   };
-  auto put = [&]() {
-    rx.put(s.X, L::LDP, t);
-    ry.put(s.dY, L::LDP, t);
-    if (t < GATES) ((float*)&s.g)[t] = rg;
+  auto put = [&](int turn) {
+    const int p0 = turn % pts * PT, st = fresh(tid) & (NT - 1);
+    const E* src = tile0 + (long)(turn / pts) * a.P + p0;
+    if (half) rt.put(s.dY, L::LDP, src, ldt, rows, min(PT, a.P - p0), vt, st);
+    else rt.template put<true>(s.X, L::LDX, src, ldt, rows, min(PT, a.P - p0), vt, st);
+    if (tid < GATES) ((float*)&s.g)[tid] = rg;
   };
-  // this wave's quarter of a state or gradient: f4 [pb][nq] holds rows p = 16 pb + g4 + j of column n
-  auto quarter = [&](f4(&v)[4][NQ], const float* from, int turn, int lane) {
+  // 16 columns q of a wave's quarter of a state or gradient: f4 [pb] holds rows p = 16 pb + g4 + j of column n
+  auto columns = [&](f4(&v)[4], const float* from, int turn, int q) {
     const float* src = from + (slot * a.H * pts + (long)h0 * pts + turn) * (long)(PT * NP);
+    const int lane = fresh(tid) & 63;
 #pragma unroll
-    for (int pb = 0; pb < 4; ++pb)
-#pragma unroll
-      for (int q = 0; q < NQ; ++q) v[pb][q] = *(const f4*)(src + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
+    for (int pb = 0; pb < 4; ++pb) v[pb] = *(const f4*)(src + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
   };
-  // dB or dC of the chunk: [n][token] accumulators of this lane's token over all n, and of all tokens over a quarter of n
+  // dB or dC of the chunk: [n][token] accumulators, of a wave's 16 tokens over all n (written to global memory), and
+  // of all tokens over its quarter of n (added through LDS)
   const long gn = (long)a.G * a.N;
-  auto half = [&](const f4(&v)[NQ][4]) {
+  auto add = [&](const f4(&v)[NQ][4]) {
+    const int lane = tid & 63, g4 = 4 * (lane >> 4), col = lane & 15;
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int b = 0; b < 4; ++b) *(f4*)(s.sum + (16 * b + col) * L::LDS_ + 16 * (w * NQ + q) + g4) = v[q][b];
   };
   auto write = [&](const f4(&v)[NB], void* whole, float* part) {
+    const int lane = tid & 63, g4 = 4 * (lane >> 4), own = 16 * w + (lane & 15);
     if (own >= rows) return;
     const bool vq = a.N % 4 == 0 && ((uintptr_t)whole & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
@@ -158,109 +158,122 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long it
   };
   fetch(0);
 
+  // Every turn: the tile and its gates into LDS (and G), barrier, the products,
+  // barrier, dx and the head's sums by waves 4 to 7, which read what they still
+  // need of the tile before the second barrier.
+  f4 acc[NB], accn[NQ][4];               // dC^T or dB^T [n][token]: of this wave's tokens, and over its quarter of n
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = zero4();
+#pragma unroll
+  for (int q = 0; q < NQ; ++q)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) accn[q][b] = zero4();
+
+  // The time steps' gradients and the sums of head h, a token a lane, by the
+  // wave with the fewest products while the next head's are formed.
+  auto finish = [&](int h) {
+    const typename L::Sums& f = s.sums[(h - h0) & 1];
+    const int lane = fresh(tid) & 63, r = lane;
+    const float A = a.A[h], step = f.dt[r];
+    const float srow = (f.srow[0][r] + f.srow[1][r]) + (f.srow[2][r] + f.srow[3][r]);
+    const float gcol = (f.gcol[0][r] + f.gcol[1][r]) + (f.gcol[2][r] + f.gcol[3][r]);
+    float dl = ((f.sg[0] + f.sg[1]) + (f.sg[2] + f.sg[3])) * f.total;
+    dl += lane_from(wave_incl_scan_dpp(lane_from(srow, 63 - lane)), 63 - lane);            // over r >= t
+    dl += before_lane(step * gcol, lane) + f.fd[r];                                        // over i < t
+#pragma unroll
+    for (int b = 1; b < 4; ++b) {
+      const float c = before_lane(r < 16 * b ? f.cs[b - 1][r] : 0.f, lane);
+      dl += r < 16 * b ? c : 0.f;
+    }
+    float raw = f.mcol[r] + f.diag[r] + gcol + A * dl;
+    const bool in = r < rows;
+    if (a.softplus) raw *= -expm1f(-step);               // sigmoid of the raw step, from its softplus
+    if (in) a.ddt[(t0 + r) * a.H + h] = raw;
+    float sa = in ? step * dl : 0.f, sd = in ? f.err[r] : 0.f, sb = in ? raw : 0.f;
+    sa = groups_sum(sum16(sa));
+    sd = groups_sum(sum16(sd));
+    sb = groups_sum(sum16(sb));
+    if (lane == 0) *(f4*)(a.sums + (slot * a.H + h) * 4) = f4{sa, sd, sb, 0.f};
+  };
+
   if (wave < 4) {
-    f4 S[4][NQ], kr[4], dct[NB], dcn[NQ][4];
-    quarter(S, a.states, 0, lane);
+    f4 S[NQ][4], G[NQ][4], kr[4];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) dct[b] = zero4();
+    for (int q = 0; q < NQ; ++q) {
+      columns(S[q], a.states, 0, q);
+      columns(G[q], a.grads, 0, q);
+    }
+    block_sync_lds();
+    {
+      const int lane = tid & 63;
+      // K of rows r = own: accumulator rows are i
 #pragma unroll
-    for (int b = 0; b < NQ; ++b)
+      for (int b = 0; b < 4; ++b) {
+        kr[b] = zero4();
+        if (b <= w)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) dcn[b][k] = zero4();
-    __syncthreads();
-    // K of rows r = own: accumulator rows are i
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      kr[b] = zero4();
-      if (b <= w)
-#pragma unroll
-        for (int k = 0; k < KN; ++k)
-          kr[b] = mma(row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane), kr[b]);
+          for (int k = 0; k < KN; ++k)
+            kr[b] = mma(row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.Cm, L::LDN, 16 * w, 32 * k, lane), kr[b]);
+      }
     }
     for (int turn = 0; turn < turns; ++turn) {
       const bool first = turn % pts == 0;
-      const int lane = fresh(lane0), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
-      put();
-      __syncthreads();
+      put(turn);
+      block_sync_lds();
+      const int lane = fresh(tid) & 63, g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+      typename L::Sums& f = s.sums[turn / pts & 1];
+      if (wave == 0) {
+        f.dt[lane] = s.g.dt[lane];
+        if (lane == 0) f.total = s.g.head[C - 1];
+      }
+      // <G, S>, then e^{b_r} S^T dy_r over this wave's quarter of n
+      {
+        float sg = 0.f;
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+          for (int pb = 0; pb < 4; ++pb)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sg += G[q][pb][j] * S[q][pb][j];
+        sg = groups_sum(sum16(sg));
+        if (lane == 0) f.sg[w] = (first ? 0.f : f.sg[w]) + sg;
+        phase();
+      }
+      float sr[4] = {};
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) {
+        Planes<E, 3> sp[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) sp[k] = planes<E, 3>(S[q][2 * k], S[q][2 * k + 1]);
+        phase();
+        if (turn + 1 < turns) {
+          columns(S[q], a.states, turn + 1, q);
+          columns(G[q], a.grads, turn + 1, q);
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          Fr<E> yf[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane);
+          const q4 c = *(const q4*)(s.Cm + (16 * b + col) * L::LDN + flip<E>(col, 16 * (w * NQ + q) + g4));
+          const float er = s.g.head[16 * b + col];
+          f4 u = zero4();
+#pragma unroll
+          for (int k = 0; k < 2; ++k) u = mma(sp[k], yf[k], u);
+          u *= er;
+          accn[q][b] += u;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sr[b] += tof(c[j]) * u[j];
+        }
+        phase();
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        sr[b] = groups_sum(sr[b]);
+        if (g4 == 0) f.srow[w][16 * b + col] = (first ? 0.f : f.srow[w][16 * b + col]) + sr[b];
+      }
+      phase();
       if (turn + 1 < turns) fetch(turn + 1);
-      const float he = s.g.bh[C - 1], le = s.g.bl[C - 1];
-      // e^{b_r} S^T dy_r over this wave's quarter of n
-      {
-        float sr[4] = {};
-#pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-          const int n0 = 16 * (w * NQ + q) + g4;
-          f4 u[4];
-#pragma unroll
-          for (int b = 0; b < 4; ++b) u[b] = zero4();
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const Planes<E, 3> sp = planes<E, 3>(S[2 * k][q], S[2 * k + 1][q]);
-#pragma unroll
-            for (int b = 0; b < 4; ++b) u[b] = mma(sp, row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), u[b]);
-          }
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const int r = 16 * b + col;
-            u[b] *= decay(s.g.bh[r], s.g.bl[r], 0.f, 0.f);
-            const f4 c = widen<E>(*(const q4*)(s.Cm + r * L::LDN + n0));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sr[b] += c[j] * u[b][j];
-            dcn[q][b] += u[b];
-          }
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          sr[b] = groups_sum(sr[b]);
-          if (g4 == 0) s.srow[w][16 * b + col] = (first ? 0.f : s.srow[w][16 * b + col]) + sr[b];
-        }
-      }
-      phase();
-      if (turn + 1 < turns) quarter(S, a.states, turn + 1, lane);
-      phase();
-      // W E diag(dt) of rows r = own: accumulator rows are i
-      f4 e[4], md = zero4();
-      {
-        const float hr = s.g.bh[own], lr = s.g.bl[own];
-        float before = 0.f;                // sum of M_ri over the blocks i < 16 w
-        Fr<E> yf[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * w, 32 * k, lane);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          e[b] = zero4();
-          if (b > w) continue;
-#pragma unroll
-          for (int k = 0; k < 2; ++k) e[b] = mma(row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), yf[k], e[b]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 16 * b + g4 + j;
-            const float f = i <= own ? e[b][j] * decay(hr, lr, s.g.bh[i], s.g.bl[i]) * s.g.dt[i] : 0.f;
-            e[b][j] = f;
-            const float m = i < own ? f * kr[b][j] : 0.f;
-            if (b == w) {
-              md[j] = m;
-            } else {
-              before += m;
-              const float c = sum16(m);
-              if (col == 0) s.cs[w - 1][i] = (first ? 0.f : s.cs[w - 1][i]) + c;
-            }
-          }
-          phase();
-        }
-        // sum over r >= t in this block and all i < t, t = own: (M V)_rt with V_it = [i < t] as a product, the
-        // blocks before as one more column, then the rows r >= t
-        before = groups_sum(before);
-        f4 v = __builtin_amdgcn_mfma_f32_16x16x4f32(g4 == 0 ? before : 0.f, 1.f, zero4(), 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x4f32(md[j], g4 + j < col ? 1.f : 0.f, v, 0, 0, 0);
-        float f = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) f += g4 + j >= col ? v[j] : 0.f;
-        f = groups_sum(f);
-        if (g4 == 0) s.fd[own] = (first ? 0.f : s.fd[own]) + f;
-      }
-      phase();
       // rows p = 16 w .. of G B^T for all tokens, to the waves that own them
       {
         f4 v[4];
@@ -268,227 +281,281 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_bwd(ScanArgs a, long it
         for (int b = 0; b < 4; ++b) v[b] = zero4();
 #pragma unroll
         for (int k = 0; k < KN; ++k) {
-          Fr<E> gp[PL];
+          Fr<E> gp[PL], bf[4];
 #pragma unroll
           for (int pl = 0; pl < PL; ++pl) gp[pl] = col_frag<E>(s.G[pl], L::LDP, 32 * k, 16 * w, lane);
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            const Fr<E> bf = row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane);
+          for (int b = 0; b < 4; ++b) bf[b] = row_frag<E>(s.B, L::LDN, 16 * b, 32 * k, lane);
+          phase();
 #pragma unroll
-            for (int pl = PL - 1; pl >= 0; --pl) v[b] = mma(gp[pl], bf, v[b]);
-          }
+          for (int pl = PL - 1; pl >= 0; --pl)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) v[b] = mma(gp[pl], bf[b], v[b]);
         }
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           const int i = 16 * b + col;
-          *(f4*)(s.dX + i * L::LDT + 16 * w + g4) = v[b] * decay(he, le, s.g.bh[i], s.g.bl[i]);
+          *(f4*)(s.dX + i * L::LDT + 16 * w + g4) = v[b] * s.g.tail[i];
         }
       }
-      __syncthreads();
+      phase();
+      // W E diag(dt) of rows r = own: accumulator rows are i
+      f4 md = zero4();
+      float before = 0.f;                // sum of M_ri over the blocks i < 16 w
+      Fr<E> yf[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (2 * k > w) break;
-        const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
+      for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * w, 32 * k, lane);
+      const float h16 = s.g.head16[own];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) dct[b] = mma(col_frag<E>(s.B, L::LDN, 32 * k, 16 * b, lane), ep, dct[b]);
+      for (int pair = 0; pair < 2; ++pair) {
+        if (2 * pair > w) break;
+        f4 e[2];
+#pragma unroll
+        for (int b2 = 0; b2 < 2; ++b2) {
+          const int b = 2 * pair + b2;
+          e[b2] = zero4();
+          if (b > w) continue;
+          Fr<E> xf[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) xf[k] = step_frag<E>(s.X, L::LDX, 16 * b, 32 * k, lane);
+          f4 wt;
+          if (b < w) {
+            wt = (h16 * between(s.g, w, b)) * *(const f4*)(s.g.tail16 + 16 * b + g4);
+          } else {
+            const f4 hi = *(const f4*)(s.g.bh + 16 * b + g4), li = *(const f4*)(s.g.bl + 16 * b + g4);
+            const float hr = s.g.bh[own], lr = s.g.bl[own];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) wt[j] = g4 + j <= col ? decay(hr, lr, hi[j], li[j]) : 0.f;
+          }
+          wt *= *(const f4*)(s.g.dt + 16 * b + g4);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) e[b2] = mma(xf[k], yf[k], e[b2]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 16 * b + g4 + j;
+            e[b2][j] = b < w || i <= own ? e[b2][j] * wt[j] : 0.f;
+            const float m = b < w || i < own ? e[b2][j] * kr[b][j] : 0.f;
+            if (b == w) {
+              md[j] = m;
+            } else {
+              before += m;
+              const float c = sum16(m);
+              if (col == 0) f.cs[w - 1][i] = (first ? 0.f : f.cs[w - 1][i]) + c;
+            }
+          }
+        }
+        const Planes<E, 2> ep = planes<E, 2>(e[0], e[1]);
+#pragma unroll
+        for (int b4 = 0; b4 < NB; b4 += 4) {
+          Fr<E> bt[4];
+#pragma unroll
+          for (int b = 0; b < 4; ++b) bt[b] = col_frag<E>(s.B, L::LDN, 32 * pair, 16 * (b4 + b), lane);
+          phase();
+#pragma unroll
+          for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) acc[b4 + b] = mma(bt[b], ep.p[pl], acc[b4 + b]);
+        }
+        phase();
       }
-      __syncthreads();
+      // sum over r >= t in this block and all i < t, t = own: (M V)_rt with V_it = [i < t] as a product, the blocks
+      // before as one more column, then the rows r >= t
+      before = groups_sum(before);
+      f4 v = __builtin_amdgcn_mfma_f32_16x16x4f32(g4 == 0 ? before : 0.f, 1.f, zero4(), 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v = __builtin_amdgcn_mfma_f32_16x16x4f32(md[j], g4 + j < col ? 1.f : 0.f, v, 0, 0, 0);
+      float m = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m += g4 + j >= col ? v[j] : 0.f;
+      m = groups_sum(m);
+      if (g4 == 0) f.fd[own] = (first ? 0.f : f.fd[own]) + m;
+      if (wave == 0 && first && turn > 0) finish(h0 + turn / pts - 1);
+      block_sync_lds();
     }
-    half(dcn);
-    __syncthreads();
-    write(dct, a.dC, a.partC);
-    __syncthreads();
-    __syncthreads();
+    if (wave == 0) finish(h1 - 1);
+    add(accn);
+    block_sync_lds();
+    write(acc, a.dC, a.partC);
+    block_sync_lds();
+    block_sync_lds();
     return;
   }
 
-  f4 G[4][NQ], kc[4], dbt[NB], dbn[NQ][4];
-  quarter(G, a.grads, 0, lane);
+  f4 G[NQ][4], kc[4];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) dbt[b] = zero4();
+  for (int q = 0; q < NQ; ++q) columns(G[q], a.grads, 0, q);
+  block_sync_lds();
+  {
+    const int lane = tid & 63;
+    // K of columns i = own: accumulator rows are r
 #pragma unroll
-  for (int b = 0; b < NQ; ++b)
+    for (int b = 0; b < 4; ++b) {
+      kc[b] = zero4();
+      if (b >= w)
 #pragma unroll
-    for (int k = 0; k < 4; ++k) dbn[b][k] = zero4();
-  __syncthreads();
-  // K of columns i = own: accumulator rows are r
-#pragma unroll
-  for (int b = 0; b < 4; ++b) {
-    kc[b] = zero4();
-    if (b >= w)
-#pragma unroll
-      for (int k = 0; k < KN; ++k)
-        kc[b] = mma(row_frag<E>(s.Cm, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.B, L::LDN, 16 * w, 32 * k, lane), kc[b]);
+        for (int k = 0; k < KN; ++k)
+          kc[b] = mma(row_frag<E>(s.Cm, L::LDN, 16 * b, 32 * k, lane), row_frag<E>(s.B, L::LDN, 16 * w, 32 * k, lane), kc[b]);
+    }
   }
   for (int turn = 0; turn < turns; ++turn) {
     const bool first = turn % pts == 0;
     const int h = h0 + turn / pts, pt = turn % pts;
-    const int lane = fresh(lane0), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
-    put();
-    float sg = 0.f;
-    {
-      const float* S = a.states + (slot * a.H * pts + (long)h0 * pts + turn) * (long)(PT * NP);
+    put(turn);
+    const int lane = fresh(tid) & 63, g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+    typename L::Sums& f = s.sums[turn / pts & 1];
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const int nn = 16 * (w * NQ + q) + col;
+    for (int q = 0; q < NQ; ++q) {
+      const int nn = 16 * (w * NQ + q) + col;
 #pragma unroll
-        for (int pb = 0; pb < 4; ++pb) {
-          f4 v = G[pb][q];
-          const f4 sv = *(const f4*)(S + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sg += v[j] * sv[j];
-#pragma unroll
-          for (int pl = 0; pl < PL; ++pl) {
-            const q4 x = narrow<E>(v);
-            *(q4*)(s.G[pl] + nn * L::LDP + 16 * pb + g4) = x;
-            if (pl + 1 < PL) v -= widen<E>(x);
-          }
-        }
-        phase();
-      }
+      for (int pb = 0; pb < 4; ++pb) put_planes<E, PL>(s.G[0] + nn * L::LDP + flip<E>(nn, 16 * pb + g4), NP * L::LDP, G[q][pb]);
     }
-    sg = groups_sum(sum16(sg));
-    if (lane == 0) s.sg[w] = (first ? 0.f : s.sg[w]) + sg;
-    __syncthreads();
-    if (turn + 1 < turns) fetch(turn + 1);
-    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1];
+    block_sync_lds();
     // e^{b_C - b_i} G^T x_i over this wave's quarter of n
-    {
-      float gc[4] = {};
+    float gc[4] = {};
 #pragma unroll
-      for (int q = 0; q < NQ; ++q) {
-        const int n0 = 16 * (w * NQ + q) + g4;
-        f4 v[4];
+    for (int q = 0; q < NQ; ++q) {
+      Planes<E, 3> gp[2];
 #pragma unroll
-        for (int b = 0; b < 4; ++b) v[b] = zero4();
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const Planes<E, 3> gp = planes<E, 3>(G[2 * k][q], G[2 * k + 1][q]);
-#pragma unroll
-          for (int b = 0; b < 4; ++b) v[b] = mma(gp, row_frag<E>(s.X, L::LDP, 16 * b, 32 * k, lane), v[b]);
-        }
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int i = 16 * b + col;
-          v[b] *= decay(he, le, s.g.bh[i], s.g.bl[i]);
-          const f4 bb = widen<E>(*(const q4*)(s.B + i * L::LDN + n0));
-#pragma unroll
-          for (int j = 0; j < 4; ++j) gc[b] += bb[j] * v[b][j];
-          dbn[q][b] += s.g.dt[i] * v[b];
-        }
-      }
+      for (int k = 0; k < 2; ++k) gp[k] = planes<E, 3>(G[q][2 * k], G[q][2 * k + 1]);
+      phase();
+      if (turn + 1 < turns) columns(G[q], a.grads, turn + 1, q);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        gc[b] = groups_sum(gc[b]);
-        if (g4 == 0) s.gcol[w][16 * b + col] = (first ? 0.f : s.gcol[w][16 * b + col]) + gc[b];
+        Fr<E> xf[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) xf[k] = step_frag<E>(s.X, L::LDX, 16 * b, 32 * k, lane);
+        const q4 c = *(const q4*)(s.B + (16 * b + col) * L::LDN + flip<E>(col, 16 * (w * NQ + q) + g4));
+        const float ei = s.g.tail[16 * b + col], dt = s.g.dt[16 * b + col];
+        f4 u = zero4();
+#pragma unroll
+        for (int k = 0; k < 2; ++k) u = mma(gp[k], xf[k], u);
+        u *= ei;
+        accn[q][b] += dt * u;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) gc[b] += tof(c[j]) * u[j];
       }
+      phase();
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      gc[b] = groups_sum(gc[b]);
+      if (g4 == 0) f.gcol[w][16 * b + col] = (first ? 0.f : f.gcol[w][16 * b + col]) + gc[b];
     }
     phase();
-    if (turn + 1 < turns) quarter(G, a.grads, turn + 1, lane);
-    phase();
+    if (turn + 1 < turns) fetch(turn + 1);
     // W E and W K of columns i = own: accumulator rows are r
     f4 xacc[4];
-    const float dt = s.g.dt[own];
-    {
-      const float hi = s.g.bh[own], li = s.g.bl[own];
-      float mcol = 0.f, diag = 0.f, err = 0.f;
-      f4 e[4], wk[4];
-      Fr<E> xf[2];
+    float mcol = 0.f, diag = 0.f, err = 0.f;
+    const float dt = s.g.dt[own], t16 = s.g.tail16[own];
+    Fr<E> xf[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) xf[k] = row_frag<E>(s.X, L::LDP, 16 * w, 32 * k, lane);
+    for (int k = 0; k < 2; ++k) xf[k] = step_frag<E>(s.X, L::LDX, 16 * w, 32 * k, lane);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        e[b] = wk[b] = zero4();
+    for (int b = 0; b < 4; ++b) xacc[b] = zero4();
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+      if (2 * pair + 1 < w) continue;
+      f4 e[2], wk[2];
+#pragma unroll
+      for (int b2 = 0; b2 < 2; ++b2) {
+        const int b = 2 * pair + b2;
+        e[b2] = wk[b2] = zero4();
         if (b < w) continue;
+        Fr<E> yf[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) e[b] = mma(row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane), xf[k], e[b]);
+        for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane);
+        f4 wt;
+        if (b > w) {
+          wt = (t16 * between(s.g, b, w)) * *(const f4*)(s.g.head16 + 16 * b + g4);
+        } else {
+          const f4 hr = *(const f4*)(s.g.bh + 16 * b + g4), lr = *(const f4*)(s.g.bl + 16 * b + g4);
+          const float hi = s.g.bh[own], li = s.g.bl[own];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) wt[j] = g4 + j >= col ? decay(hr[j], lr[j], hi, li) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) e[b2] = mma(yf[k], xf[k], e[b2]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int r = 16 * b + g4 + j;
-          const float wt = r >= own ? decay(s.g.bh[r], s.g.bl[r], hi, li) : 0.f;
-          const float ev = r >= own ? e[b][j] : 0.f, f = ev * wt;
-          mcol += r > own ? f * kc[b][j] : 0.f;
-          diag += r == own ? ev * kc[b][j] : 0.f;
-          err += r == own ? ev : 0.f;
-          e[b][j] = f * dt;
-          wk[b][j] = r >= own ? wt * kc[b][j] : 0.f;
+          const bool in = b > w || r >= own;
+          const float ev = in ? e[b2][j] : 0.f, we = ev * wt[j];
+          if (b > w) {
+            mcol += we * kc[b][j];
+          } else {
+            mcol += r > own ? we * kc[b][j] : 0.f;
+            diag += r == own ? ev * kc[b][j] : 0.f;
+            err += r == own ? ev : 0.f;
+          }
+          e[b2][j] = we * dt;
+          wk[b2][j] = in ? wt[j] * kc[b][j] : 0.f;
         }
-        phase();
       }
-      mcol = groups_sum(mcol);
-      diag = groups_sum(diag);
-      err = groups_sum(err);
-      if (g4 == 0) {
-        s.mcol[own] = (first ? 0.f : s.mcol[own]) + mcol;
-        s.diag[own] = (first ? 0.f : s.diag[own]) + diag;
-        s.err[own] = (first ? 0.f : s.err[own]) + err;
+      {
+        const Planes<E, 2> wp = planes<E, 2>(wk[0], wk[1]);
+        Fr<E> yt[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) yt[b] = col_frag<E>(s.dY, L::LDP, 32 * pair, 16 * b, lane);
+        phase();
+#pragma unroll
+        for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) xacc[b] = mma(yt[b], wp.p[pl], xacc[b]);
+      }
+      const Planes<E, 2> ep = planes<E, 2>(e[0], e[1]);
+#pragma unroll
+      for (int b4 = 0; b4 < NB; b4 += 4) {
+        Fr<E> ct[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) ct[b] = col_frag<E>(s.Cm, L::LDN, 32 * pair, 16 * (b4 + b), lane);
+        phase();
+#pragma unroll
+        for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) acc[b4 + b] = mma(ct[b], ep.p[pl], acc[b4 + b]);
       }
       phase();
-#pragma unroll
-      for (int b = 0; b < 4; ++b) xacc[b] = zero4();
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (2 * k + 1 < w) continue;
-        const Planes<E, 2> ep = planes<E, 2>(e[2 * k], e[2 * k + 1]);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dbt[b] = mma(col_frag<E>(s.Cm, L::LDN, 32 * k, 16 * b, lane), ep, dbt[b]);
-        const Planes<E, 2> wp = planes<E, 2>(wk[2 * k], wk[2 * k + 1]);
-#pragma unroll
-        for (int b = 0; b < 4; ++b) xacc[b] = mma(col_frag<E>(s.dY, L::LDP, 32 * k, 16 * b, lane), wp, xacc[b]);
-      }
     }
-    __syncthreads();
+    mcol = groups_sum(mcol);
+    diag = groups_sum(diag);
+    err = groups_sum(err);
+    if (g4 == 0) {
+      f.mcol[own] = (first ? 0.f : f.mcol[own]) + mcol;
+      f.diag[own] = (first ? 0.f : f.diag[own]) + diag;
+      f.err[own] = (first ? 0.f : f.err[own]) + err;
+    }
+    q4 dq[4];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) dq[b] = *(const q4*)(s.dY + own * L::LDP + flip<E>(col, 16 * b + g4));
+    block_sync_lds();
     {
       const int cols = min(PT, a.P - pt * PT);
       const float D = a.D ? a.D[h] : 0.f;
-      E* out = (E*)a.dx + ((t0 + own) * a.H + h) * (long)a.P + pt * PT;
-      const bool vo = a.P % 4 == 0 && ((uintptr_t)a.dx & (4 * sizeof(E) - 1)) == 0;
-      if (own < rows)
+      E* out = (E*)a.dx + t0 * ldy + (long)h * a.P + pt * PT;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          const int p = 16 * b + g4;
-          f4 v = dt * (xacc[b] + *(const f4*)(s.dX + own * L::LDT + p));
-          if (a.D) v += D * widen<E>(*(const q4*)(s.dY + own * L::LDP + p));
-          if (vo) {
-            if (p < cols) *(q4*)(out + p) = narrow<E>(v);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (p + j < cols) out[p + j] = fromf<E>(v[j]);
-          }
-        }
-    }
-    // the time step's gradient and the head's sums, a token a lane, on the wave with the fewest products
-    if (pt == pts - 1 && w == 3) {
-      const int r = lane;
-      const float step = s.g.dt[r], A = a.A[h];
-      const float srow = (s.srow[0][r] + s.srow[1][r]) + (s.srow[2][r] + s.srow[3][r]);
-      const float gcol = (s.gcol[0][r] + s.gcol[1][r]) + (s.gcol[2][r] + s.gcol[3][r]);
-      float dl = ((s.sg[0] + s.sg[1]) + (s.sg[2] + s.sg[3])) * decay(he, le, 0.f, 0.f);
-      dl += lane_from(wave_incl_scan_dpp(lane_from(srow, 63 - lane)), 63 - lane);          // over r >= t
-      dl += before_lane(step * gcol, lane) + s.fd[r];                                      // over i < t
-#pragma unroll
-      for (int b = 1; b < 4; ++b) {
-        const float c = before_lane(r < 16 * b ? s.cs[b - 1][r] : 0.f, lane);
-        dl += r < 16 * b ? c : 0.f;
+      for (int b = 0; b < 4; ++b) {
+        xacc[b] = dt * (xacc[b] + *(const f4*)(s.dX + own * L::LDT + 16 * b + g4));
+        if (a.D) xacc[b] += D * widen<E>(dq[b]);
       }
-      float raw = s.mcol[r] + s.diag[r] + gcol + A * dl;
-      const bool in = r < rows;
-      if (a.softplus) raw *= -expm1f(-step);             // sigmoid of the raw step, from its softplus
-      if (in) a.ddt[(t0 + r) * a.H + h] = raw;
-      float sa = in ? step * dl : 0.f, sd = in ? s.err[r] : 0.f, sb = in ? raw : 0.f;
-      sa = groups_sum(sum16(sa));
-      sd = groups_sum(sum16(sd));
-      sb = groups_sum(sum16(sb));
-      if (lane == 0) *(f4*)(a.sums + (slot * a.H + h) * 4) = f4{sa, sd, sb, 0.f};
+      if (__builtin_expect(quad_rows<E>(out, ldy, cols), 1)) {
+        const __amdgpu_buffer_rsrc_t buf = buffer(uniform_ptr(out), (uint32_t)(rows * ldy) * (uint32_t)sizeof(E));
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          store_quad<E>(buf, 16 * b + g4 < cols ? (uint32_t)(own * ldy + 16 * b + g4) * (uint32_t)sizeof(E) : 0x80000000u, xacc[b]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (own < rows && 16 * b + g4 + j < cols) out[own * ldy + 16 * b + g4 + j] = fromf<E>(xacc[b][j]);
+      }
     }
-    __syncthreads();
   }
-  __syncthreads();
-  __syncthreads();
-  half(dbn);
-  __syncthreads();
-  write(dbt, a.dB, a.partB);
+  block_sync_lds();
+  block_sync_lds();
+  add(accn);
+  block_sync_lds();
+  write(acc, a.dB, a.partB);
 }
 
 // dB and dC from the shares of the splits, in order.

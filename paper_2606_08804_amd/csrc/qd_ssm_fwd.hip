@@ -48,6 +48,12 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
     g[0] = dt;
     g[C] = (float)b;
     g[2 * C] = (float)(b - (double)(float)b);
+    // each from a difference formed in 64 bits
+    const double before = __shfl(b, max(lane & ~15, 1) - 1, 64);
+    g[3 * C] = fast_exp((float)b);
+    g[4 * C] = fast_exp((float)(__shfl(b, C - 1, 64) - b));
+    g[5 * C] = fast_exp((float)(lane < 16 ? b : b - before));
+    g[6 * C] = fast_exp((float)(__shfl(b, lane | 15, 64) - b));
   }
 }
 
@@ -64,10 +70,12 @@ __device__ inline bool not_finite(u32x4 v) {
 // Operands of a chunk in LDS; rows and columns outside the matrices are zeros.
 template <typename E, int NP>
 struct OutLds {
-  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDC = lds_ld<E>(C), PL = sizeof(E) == 2 ? 2 : 1;
+  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDM = steps_ld<E>(NP), LDC = steps_ld<E>(C),
+                       PL = sizeof(E) == 2 ? 2 : 1;
   struct Buf {
-    E B[C * LDN], Cm[C * LDN], X[C * LDP];
-    E W[PL][C * LDC];                  // W o C B^T diag(dt), [r][i], planes
+    E B[C * LDN], X[C * LDP];
+    E Cm[C * LDM];                     // steps
+    E W[PL][C * LDC];                  // W o C B^T diag(dt), [r][i], planes; steps
     Gates g;
   };
   static constexpr int NBUF = 2 * sizeof(Buf) + 64 <= 163840 ? 2 : 1;
@@ -81,7 +89,7 @@ struct OutLds {
 // barriers, after the operands are in LDS and at the end.  fp32 with N > 64
 // has room for one chunk in LDS only: there the two halves take turns.
 template <typename E, int NP>
-__global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long items) {
+__global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanArgs a, long items) {
   typedef OutLds<E, NP> L;
   typedef typename Q4<E>::t q4;
   __shared__ __attribute__((aligned(16))) L s;
@@ -101,8 +109,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
     return;
   }
   const int end = whole ? len : min(pos + a.seg, len), chunks = (end - pos + C - 1) / C;
-  const int t = threadIdx.x & (NTHREADS - 1), lane = t & 63, wave = wave_id(threadIdx.x), w = wave & 3;
-  const int g4 = 4 * (lane >> 4), col = lane & 15;
+  const int t_ = threadIdx.x & (NTHREADS - 1), t = t_, wave = wave_id(threadIdx.x), w = wave & 3;
   const int cols = min(PT, a.P - p0), grp = h / (a.H / a.G);
 
   if (wave >= 4) {
@@ -113,21 +120,25 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
     const long cslot = (a.q.cu ? s0 / C + n : (long)n * ((a.q.T + C - 1) / C)) + pos / C;
     Stage<E, PT, NTHREADS> rx;
     Stage<E, NP, NTHREADS> rb, rc;
-    float rg = 0.f;
+    float rg[2];
+    const uint32_t ox = rx.offset(a.ldx, cols, t), ob = rb.offset(a.ldb, a.N, t), oc = rc.offset(a.ldc, a.N, t);
     auto fetch = [&](int c) {
       const int rows = min(C, end - pos - c * C);
-      rx.load(x + (long)c * C * a.ldx, a.ldx, rows, cols, vx, t);
-      rb.load(B + (long)c * C * a.ldb, a.ldb, rows, a.N, vb, t);
-      rc.load(Cm + (long)c * C * a.ldc, a.ldc, rows, a.N, vc, t);
-      if (t < GATES) rg = a.gates[((cslot + c) * a.H + h) * GATES + t];
+      rx.load(x + (long)c * C * a.ldx, a.ldx, rows, vx, ox);
+      rb.load(B + (long)c * C * a.ldb, a.ldb, rows, vb, ob);
+      rc.load(Cm + (long)c * C * a.ldc, a.ldc, rows, vc, oc);
+      rg[0] = load_gate(a.gates + ((cslot + c) * a.H + h) * GATES, t);
+      rg[1] = load_gate(a.gates + ((cslot + c) * a.H + h) * GATES, NTHREADS + t);
     };
     auto put = [&](int c) {
       typename L::Buf& u = s.buf[c % NBUF];
-      rx.put(u.X, L::LDP, t);
-      rb.put(u.B, L::LDN, t);
-      rc.put(u.Cm, L::LDN, t);
-      if (t < GATES) ((float*)&u.g)[t] = rg;
-      bool bad = false;
+      const int t = fresh(t_), rows = min(C, end - pos - c * C);
+      rx.put(u.X, L::LDP, x + (long)c * C * a.ldx, a.ldx, rows, cols, vx, t);
+      rb.put(u.B, L::LDN, B + (long)c * C * a.ldb, a.ldb, rows, a.N, vb, t);
+      rc.template put<true>(u.Cm, L::LDM, Cm + (long)c * C * a.ldc, a.ldc, rows, a.N, vc, t);
+      ((float*)&u.g)[t] = rg[0];
+      if (t < GATES - NTHREADS) ((float*)&u.g)[NTHREADS + t] = rg[1];
+      bool bad = !vx;                    // not looked at: the consumers do
 #pragma unroll
       for (int k = 0; k < rx.K; ++k) bad |= not_finite<E>(rx.r[k]);
       if (bad) s.bad[c & 1] = c + 1;
@@ -135,57 +146,68 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
     // rows r = 16 w + col, formed as their transposes: accumulator rows are i
     auto scores = [&](int c) {
       typename L::Buf& u = s.buf[c % NBUF];
+      const int lane = fresh(t_) & 63, g4 = 4 * (lane >> 4), col = lane & 15;
       Fr<E> cf[KN];
 #pragma unroll
-      for (int k = 0; k < KN; ++k) cf[k] = row_frag<E>(u.Cm, L::LDN, 16 * w, 32 * k, lane);
+      for (int k = 0; k < KN; ++k) cf[k] = step_frag<E>(u.Cm, L::LDM, 16 * w, 32 * k, lane);
       const int r = 16 * w + col;
       const float hr = u.g.bh[r], lr = u.g.bl[r];
 #pragma unroll
-      for (int ib = 0; ib < 4; ++ib) {
-        if (ib > (w | 1)) break;         // products take blocks in pairs: the one beside the last is zero
-        f4 v = zero4();
-        if (ib <= w) {
+      for (int pair = 0; pair < 2; ++pair) {       // products take blocks of i in pairs
+        if (2 * pair > w) break;
+        Fr<E> bf[2][KN];
+        f4 hi[2], li[2], dt[2], v[2];
 #pragma unroll
-          for (int k = 0; k < KN; ++k) v = mma(row_frag<E>(u.B, L::LDN, 16 * ib, 32 * k, lane), cf[k], v);
+        for (int b = 0; b < 2; ++b) {
+          const int i0 = 32 * pair + 16 * b;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int i = 16 * ib + g4 + j;
-            v[j] = i <= r ? v[j] * decay(hr, lr, u.g.bh[i], u.g.bl[i]) * u.g.dt[i] : 0.f;
-          }
+          for (int k = 0; k < KN; ++k) bf[b][k] = row_frag<E>(u.B, L::LDN, i0, 32 * k, lane);
+          hi[b] = *(const f4*)(u.g.bh + i0 + g4);
+          li[b] = *(const f4*)(u.g.bl + i0 + g4);
+          dt[b] = *(const f4*)(u.g.dt + i0 + g4);
+          v[b] = zero4();
         }
+        phase();
 #pragma unroll
-        for (int pl = 0; pl < PL; ++pl) {
-          const q4 q = narrow<E>(v);
-          *(q4*)(u.W[pl] + r * L::LDC + 16 * ib + g4) = q;
-          if (pl + 1 < PL) v -= widen<E>(q);
+        for (int k = 0; k < KN; ++k)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) v[b] = mma(bf[b][k], cf[k], v[b]);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int i0 = 32 * pair + 16 * b;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            v[b][j] = i0 + g4 + j <= r ? v[b][j] * (decay(hr, lr, hi[b][j], li[b][j]) * dt[b][j]) : 0.f;
+          put_planes<E, PL>(u.W[0] + r * L::LDC + step_at<E>(i0 + g4), C * L::LDC, v[b]);
         }
       }
     };
     if (t < 2) s.bad[t] = 0;
     if (chunks > 0) fetch(0);
-    __syncthreads();
+    block_sync_lds();
     if (chunks > 0) put(0);
     if (chunks > 1) fetch(1);
-    __syncthreads();
+    block_sync_lds();
     if (chunks > 0) scores(0);
-    __syncthreads();
+    block_sync_lds();
     for (int c = 0; c < chunks; ++c) {
-      if (NBUF == 1) __syncthreads();    // the consumers have read this chunk
+      if (NBUF == 1) block_sync_lds();    // the consumers have read this chunk
       const bool more = c + 1 < chunks;
       if (more) put(c + 1);
-      __syncthreads();
+      block_sync_lds();
       if (c + 2 < chunks) fetch(c + 2);
       if (more) scores(c + 1);
-      __syncthreads();
+      block_sync_lds();
     }
     return;
   }
 
+  const long ldy = (long)a.H * a.P;
   E* y = (E*)a.y + ((s0 + pos) * a.H + h) * (long)a.P + p0;
-  const bool vy = a.P % 4 == 0 && ((uintptr_t)a.y & (4 * sizeof(E) - 1)) == 0;
+  const bool vy = quad_rows<E>(y, ldy, cols);
   const float D = a.D ? a.D[h] : 0.f;
   // state: f4 S[nb] holds n = 16 nb + g4 + j of row p = p0 + 16 w + col
-  const int p = p0 + 16 * w + col;
+  const int p = p0 + 16 * w + (t & 15), g4_ = 4 * ((t & 63) >> 4);
   const float* in = whole ? (a.S0 ? a.S0 + ((long)n * a.H + h) * a.P * a.N : nullptr)
                           : a.entry[0] + (slot * a.H + h) * (long)a.P * a.N;
   f4 S[NB];
@@ -193,22 +215,33 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
   for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int nn = 16 * nb + g4 + j;
+      const int nn = 16 * nb + g4_ + j;
       S[nb][j] = in && p < a.P && nn < a.N ? in[(long)p * a.N + nn] : 0.f;
     }
-  __syncthreads();
-  __syncthreads();
-  __syncthreads();
+  block_sync_lds();
+  block_sync_lds();
+  block_sync_lds();
+  // operands with C, read a chunk ahead where there is room
+  constexpr bool AHEAD = NBUF == 2 && sizeof(E) == 2;
+  Fr<E> cf[AHEAD ? KN : 1][4];
+  auto read_c = [&](int c, int lane) {
+#pragma unroll
+    for (int k = 0; k < KN; ++k)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) cf[AHEAD ? k : 0][b] = step_frag<E>(s.buf[c % NBUF].Cm, L::LDM, 16 * b, 32 * k, lane);
+  };
+  if (AHEAD && chunks > 0) read_c(0, t & 63);
   for (int c = 0; c < chunks; ++c) {
     const typename L::Buf& u = s.buf[c % NBUF];
     const int rows = min(C, end - pos - c * C);
+    const int lane = fresh(t_) & 63, g4 = 4 * (lane >> 4), col = lane & 15;
     Fr<E> xt[2];                         // x^T: row p, k = i
 #pragma unroll
     for (int k = 0; k < 2; ++k) xt[k] = col_frag<E>(u.X, L::LDP, 32 * k, 16 * w, lane);
     // An infinity or a NaN in x must not meet the zero weights of the tokens
     // before it: it is taken out, and what it enters becomes NaN.
     int first = C;                       // token of row p's first one
-    if (s.bad[c & 1] == c + 1) {
+    if (__builtin_expect(s.bad[c & 1] == c + 1, 0)) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         f4 v[2];
@@ -228,66 +261,113 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
     }
     // Y^T: rows p, columns r
     f4 o[4];
+    float er[4];
+    Fr<E> wf[2][4][PL];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) o[b] = zero4();
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int k = 0; k < KN; ++k) {
-      const Planes<E, 2> sp = planes<E, 2>(S[2 * k], S[2 * k + 1]);
+      for (int b = 2 * k; b < 4; ++b)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) o[b] = mma(sp, row_frag<E>(u.Cm, L::LDN, 16 * b, 32 * k, lane), o[b]);
-    }
+        for (int pl = 0; pl < PL; ++pl) wf[k][b][pl] = step_frag<E>(u.W[pl], L::LDC, 16 * b, 32 * k, lane);
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
-      const int r = 16 * b + col;
-      o[b] *= decay(u.g.bh[r], u.g.bl[r], 0.f, 0.f);
+      o[b] = zero4();
+      er[b] = u.g.head[16 * b + col];
+    }
+    q4 xd[4];
 #pragma unroll
-      for (int k = 0; k <= b / 2; ++k)
+    for (int b = 0; b < 4; ++b) xd[b] = *(const q4*)(u.X + (16 * b + col) * L::LDP + flip<E>(col, 16 * w + g4));
+    phase();
 #pragma unroll
-        for (int pl = PL - 1; pl >= 0; --pl)
-          o[b] = mma(xt[k], row_frag<E>(u.W[pl], L::LDC, 16 * b, 32 * k, lane), o[b]);
-      if (a.D) o[b] += D * widen<E>(*(const q4*)(u.X + r * L::LDP + 16 * w + g4));
-      if (s.bad[c & 1] == c + 1)
+    for (int k = 0; k < KN; ++k) {
+      if (!AHEAD) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) cf[0][b] = step_frag<E>(u.Cm, L::LDM, 16 * b, 32 * k, lane);
+        phase();
+      }
+      const Planes<E, 2> sp = planes<E, 2>(S[2 * k], S[2 * k + 1]);
+#pragma unroll
+      for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) o[b] = mma(sp.p[pl], cf[AHEAD ? k : 0][b], o[b]);
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) o[b] *= er[b];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int pl = PL - 1; pl >= 0; --pl)
+#pragma unroll
+        for (int b = 2 * k; b < 4; ++b) o[b] = mma(xt[k], wf[k][b][pl], o[b]);
+    phase();
+    if (NBUF == 2) block_sync_lds();
+    // operands of the state's update, in flight over the outputs
+    Fr<E> bt[2][NB];
+    auto read_b = [&](int k) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) bt[k][nb] = col_frag<E>(u.B, L::LDN, 32 * k, 16 * nb, lane);
+    };
+    read_b(0);
+    if (sizeof(E) == 2) read_b(1);
+    f4 ws[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        ws[k][i] = *(const f4*)(u.g.dt + 32 * k + 16 * i + g4) * *(const f4*)(u.g.tail + 32 * k + 16 * i + g4);
+    const float total = u.g.head[C - 1];
+    phase();
+    if (a.D)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) o[b] += D * widen<E>(xd[b]);
+    if (__builtin_expect(s.bad[c & 1] == c + 1, 0))
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (r >= __shfl(first, g4 + j, 64)) o[b][j] = __builtin_nanf("");
-      if (r < rows) {
-        const int pc = 16 * w + g4;
-        E* out = y + (long)(c * C + r) * a.H * a.P + pc;
-        if (vy) {
-          if (pc < cols) *(q4*)out = narrow<E>(o[b]);
-        } else {
+          if (16 * b + col >= __shfl(first, g4 + j, 64)) o[b][j] = __builtin_nanf("");
+    {
+      const int pc = 16 * w + g4;
+      E* out = y + (long)c * C * ldy;
+      if (__builtin_expect(vy, 1)) {
+        const __amdgpu_buffer_rsrc_t buf = buffer(uniform_ptr(out), (uint32_t)(rows * ldy) * (uint32_t)sizeof(E));
+        const uint32_t off = pc < cols ? (uint32_t)(col * ldy + pc) * (uint32_t)sizeof(E) : 0x80000000u;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) store_quad<E>(buf, off + (uint32_t)(16 * b * ldy) * (uint32_t)sizeof(E), o[b]);
+      } else {
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (pc + j < cols) out[j] = fromf<E>(o[b][j]);
-        }
+            if (16 * b + col < rows && pc + j < cols) out[(16 * b + col) * ldy + pc + j] = fromf<E>(o[b][j]);
       }
     }
-    if (NBUF == 2) __syncthreads();
     // S': rows n, columns p
-    const float he = u.g.bh[C - 1], le = u.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) S[nb] *= total;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
+      if (sizeof(E) != 2 && k) {
+        read_b(1);
+        phase();
+      }
       f4 v[2];
       quads<E>(xt[k], v[0], v[1]);
+      const Planes<E, 3> xw = planes<E, 3>(v[0] * ws[k][0], v[1] * ws[k][1]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int r = 32 * k + 16 * (i / 4) + g4 + i % 4;
-        v[i / 4][i % 4] *= u.g.dt[r] * decay(he, le, u.g.bh[r], u.g.bl[r]);
-      }
-      const Planes<E, 3> xw = planes<E, 3>(v[0], v[1]);
+      for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(col_frag<E>(u.B, L::LDN, 32 * k, 16 * nb, lane), xw, S[nb]);
+        for (int nb = 0; nb < NB; ++nb) S[nb] = mma(bt[k][nb], xw.p[pl], S[nb]);
     }
+    if (AHEAD && c + 1 < chunks) read_c(c + 1, lane);
     if (first < C)
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) S[nb] = zero4() + __builtin_nanf("");
     if (NBUF == 1) {
-      __syncthreads();
-      __syncthreads();
+      block_sync_lds();
+      block_sync_lds();
     }
-    __syncthreads();
+    block_sync_lds();
   }
   if (whole && a.Sf && p < a.P) {
     float* out = a.Sf + (((long)n * a.H + h) * a.P + p) * a.N;
@@ -295,7 +375,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) void k_ssm_out(ScanArgs a, long it
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        if (16 * nb + g4 + j < a.N) out[16 * nb + g4 + j] = S[nb][j];
+        if (16 * nb + g4_ + j < a.N) out[16 * nb + g4_ + j] = S[nb][j];
   }
 }
 
@@ -312,7 +392,7 @@ struct WalkLds {
 };
 
 template <typename E, int NP>
-__global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items, int dir0, int keep) {
+__global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs a, long items, int dir0, int keep) {
   typedef WalkLds<E, NP> L;
   __shared__ __attribute__((aligned(16))) L s;
   constexpr int NB = NP / 16;
@@ -358,12 +438,14 @@ __global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items
 
   Stage<E, PT, NTHREADS> rx;
   Stage<E, NP, NTHREADS> rb;
-  float rg = 0.f;
+  float rg[2];
+  const uint32_t ox = rx.offset(ldx, cols, t), ob = rb.offset(ldb, a.N, t);
   auto fetch = [&](int c) {
     const int rows = min(C, end - pos - c * C);
-    rx.load(x + (long)c * C * ldx, ldx, rows, cols, vx, t);
-    rb.load(B + (long)c * C * ldb, ldb, rows, a.N, vb, t);
-    if (t < GATES) rg = a.gates[((cslot + c) * a.H + h) * GATES + t];
+    rx.load(x + (long)c * C * ldx, ldx, rows, vx, ox);
+    rb.load(B + (long)c * C * ldb, ldb, rows, vb, ob);
+    rg[0] = load_gate(a.gates + ((cslot + c) * a.H + h) * GATES, t);
+    rg[1] = load_gate(a.gates + ((cslot + c) * a.H + h) * GATES, NTHREADS + t);
   };
   if (chunks > 0) fetch(dir ? chunks - 1 : 0);
   for (int k0 = 0; k0 < chunks; ++k0) {
@@ -373,36 +455,51 @@ __global__ __launch_bounds__(NTHREADS, 2) void k_ssm_walk(ScanArgs a, long items
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) *(f4*)(out + ((w * NB + nb) * 64 + lane) * 4) = S[nb];
     }
-    rx.put(s.X, L::LDP, t);
-    rb.put(s.B, L::LDN, t);
-    if (t < GATES) ((float*)&s.g)[t] = rg;
-    __syncthreads();
+    {
+      const int rows = min(C, end - pos - c * C);
+      rx.put(s.X, L::LDP, x + (long)c * C * ldx, ldx, rows, cols, vx, t);
+      rb.put(s.B, L::LDN, B + (long)c * C * ldb, ldb, rows, a.N, vb, t);
+    }
+    ((float*)&s.g)[t] = rg[0];
+    if (t < GATES - NTHREADS) ((float*)&s.g)[NTHREADS + t] = rg[1];
+    block_sync_lds();
     if (k0 + 1 < chunks) fetch(dir ? c - 1 : c + 1);
-    const float he = s.g.bh[C - 1], le = s.g.bl[C - 1], total = decay(he, le, 0.f, 0.f);
-    run += (double)he + (double)le;
+    const float total = s.g.head[C - 1];
+    run += (double)s.g.bh[C - 1] + (double)s.g.bl[C - 1];
+    Fr<E> xt[2], bt[2][NB];
+    f4 ws[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      xt[k] = col_frag<E>(s.X, L::LDP, 32 * k, 16 * w, lane);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int at = 32 * k + 16 * i + g4;
+        ws[k][i] = dir ? *(const f4*)(s.g.head + at) : *(const f4*)(s.g.dt + at) * *(const f4*)(s.g.tail + at);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < (sizeof(E) == 2 ? 2 : 1); ++k)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) bt[k][nb] = col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane);
+    phase();
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) S[nb] *= total;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const Fr<E> xt = col_frag<E>(s.X, L::LDP, 32 * k, 16 * w, lane);
-      f4 u, v;
-      quads<E>(xt, u, v);
+      f4 v[2];
+      quads<E>(xt[k], v[0], v[1]);
+      const Planes<E, 3> xw = planes<E, 3>(v[0] * ws[k][0], v[1] * ws[k][1]);
+      if (sizeof(E) != 2 && k) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 32 * k + g4 + j, i2 = i + 16;
-        if (dir) {
-          u[j] *= decay(s.g.bh[i], s.g.bl[i], 0.f, 0.f);
-          v[j] *= decay(s.g.bh[i2], s.g.bl[i2], 0.f, 0.f);
-        } else {
-          u[j] *= s.g.dt[i] * decay(he, le, s.g.bh[i], s.g.bl[i]);
-          v[j] *= s.g.dt[i2] * decay(he, le, s.g.bh[i2], s.g.bl[i2]);
-        }
+        for (int nb = 0; nb < NB; ++nb) bt[k][nb] = col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane);
+        phase();
       }
-      const Planes<E, 3> xw = planes<E, 3>(u, v);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) S[nb] = mma(xw, col_frag<E>(s.B, L::LDN, 32 * k, 16 * nb, lane), S[nb]);
+      for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) S[nb] = mma(xw.p[pl], bt[k][nb], S[nb]);
     }
-    __syncthreads();
+    block_sync_lds();
   }
   float* out = whole ? (dir ? a.dS0 : nullptr) : keep ? nullptr : a.total[dir];
   if (whole && out) out += ((long)n * a.H + h) * a.P * a.N;

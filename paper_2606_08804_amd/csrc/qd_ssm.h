@@ -246,12 +246,14 @@ inline unsigned xcd_grid(long n) { return (unsigned)((n + 7) / 8 * 8); }
 __device__ inline void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // The lane number as a value the compiler cannot trace: what is formed from it
-// (LDS addresses, masks of the triangles) is formed again every turn of a
-// loop instead of being kept in registers, which are all taken (hoisted, 130
-// such values went to scratch memory and back).
-__device__ inline int fresh(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
+// (LDS addresses, masks of the triangles) is formed again every turn of a loop
+// instead of being kept in registers, which are all taken (hoisted, 130 such
+// values went to scratch memory and back).  Counted from the hardware's lane
+// mask, it takes no register between turns either.
+__device__ inline int fresh_lane() {
+  uint32_t zero = 0;
+  asm volatile("" : "+s"(zero));
+  return (int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
 }
 
 // A tile of 64 rows x COLS staged through registers: loads first, LDS later.

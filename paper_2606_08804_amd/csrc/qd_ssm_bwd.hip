@@ -104,21 +104,21 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
   // whole pieces in one tile of a head are whole pieces in all of them
   const bool vt = a.P % (16 / (int)sizeof(E)) == 0 && vec_rows<E>(tile0, ldt, a.P);
   auto fetch = [&](int turn) {
-    const int p0 = turn % pts * PT, st = fresh(tid) & (NT - 1);
+    const int p0 = turn % pts * PT, st = (wave & 3) * 64 + fresh_lane();
     rt.load(tile0 + (long)(turn / pts) * a.P + p0, ldt, rows, vt, rt.offset(ldt, min(PT, a.P - p0), st));
-    rg = load_gate(a.gates + (slot * a.H + h0 + turn / pts) * GATES, tid);
+    rg = load_gate(a.gates + (slot * a.H + h0 + turn / pts) * GATES, half * NT + st);
   };
   auto put = [&](int turn) {
-    const int p0 = turn % pts * PT, st = fresh(tid) & (NT - 1);
+    const int p0 = turn % pts * PT, st = (wave & 3) * 64 + fresh_lane();
     const E* src = tile0 + (long)(turn / pts) * a.P + p0;
     if (half) rt.put(s.dY, L::LDP, src, ldt, rows, min(PT, a.P - p0), vt, st);
     else rt.template put<true>(s.X, L::LDX, src, ldt, rows, min(PT, a.P - p0), vt, st);
-    if (tid < GATES) ((float*)&s.g)[tid] = rg;
+    if (half * NT + st < GATES) ((float*)&s.g)[half * NT + st] = rg;
   };
   // 16 columns q of a wave's quarter of a state or gradient: f4 [pb] holds rows p = 16 pb + g4 + j of column n
   auto columns = [&](f4(&v)[4], const float* from, int turn, int q) {
     const float* src = from + (slot * a.H * pts + (long)h0 * pts + turn) * (long)(PT * NP);
-    const int lane = fresh(tid) & 63;
+    const int lane = fresh_lane();
 #pragma unroll
     for (int pb = 0; pb < 4; ++pb) v[pb] = *(const f4*)(src + ((pb * NB + w * NQ + q) * 64 + lane) * 4);
   };
@@ -126,14 +126,14 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
   // of all tokens over its quarter of n (added through LDS)
   const long gn = (long)a.G * a.N;
   auto add = [&](const f4(&v)[NQ][4]) {
-    const int lane = tid & 63, g4 = 4 * (lane >> 4), col = lane & 15;
+    const int lane = fresh_lane(), g4 = 4 * (lane >> 4), col = lane & 15;
 #pragma unroll
     for (int q = 0; q < NQ; ++q)
 #pragma unroll
       for (int b = 0; b < 4; ++b) *(f4*)(s.sum + (16 * b + col) * L::LDS_ + 16 * (w * NQ + q) + g4) = v[q][b];
   };
   auto write = [&](const f4(&v)[NB], void* whole, float* part) {
-    const int lane = tid & 63, g4 = 4 * (lane >> 4), own = 16 * w + (lane & 15);
+    const int lane = fresh_lane(), g4 = 4 * (lane >> 4), own = 16 * w + (lane & 15);
     if (own >= rows) return;
     const bool vq = a.N % 4 == 0 && ((uintptr_t)whole & (4 * sizeof(E) - 1)) == 0;
 #pragma unroll
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
   // wave with the fewest products while the next head's are formed.
   auto finish = [&](int h) {
     const typename L::Sums& f = s.sums[(h - h0) & 1];
-    const int lane = fresh(tid) & 63, r = lane;
+    const int lane = fresh_lane(), r = lane;
     const float A = a.A[h], step = f.dt[r];
     const float srow = (f.srow[0][r] + f.srow[1][r]) + (f.srow[2][r] + f.srow[3][r]);
     const float gcol = (f.gcol[0][r] + f.gcol[1][r]) + (f.gcol[2][r] + f.gcol[3][r]);
@@ -205,7 +205,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
     }
     block_sync_lds();
     {
-      const int lane = tid & 63;
+      const int lane = fresh_lane();
       // K of rows r = own: accumulator rows are i
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
@@ -218,9 +218,10 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
     }
     for (int turn = 0; turn < turns; ++turn) {
       const bool first = turn % pts == 0;
+      const int next = min(turn + 1, turns - 1);      // the last turn loads itself again: no branch around the loads
       put(turn);
       block_sync_lds();
-      const int lane = fresh(tid) & 63, g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+      const int lane = fresh_lane(), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
       typename L::Sums& f = s.sums[turn / pts & 1];
       if (wave == 0) {
         f.dt[lane] = s.g.dt[lane];
@@ -246,10 +247,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
 #pragma unroll
         for (int k = 0; k < 2; ++k) sp[k] = planes<E, 3>(S[q][2 * k], S[q][2 * k + 1]);
         phase();
-        if (turn + 1 < turns) {
-          columns(S[q], a.states, turn + 1, q);
-          columns(G[q], a.grads, turn + 1, q);
-        }
+        columns(S[q], a.states, next, q);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           Fr<E> yf[2];
@@ -273,7 +271,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
         if (g4 == 0) f.srow[w][16 * b + col] = (first ? 0.f : f.srow[w][16 * b + col]) + sr[b];
       }
       phase();
-      if (turn + 1 < turns) fetch(turn + 1);
+      fetch(next);
       // rows p = 16 w .. of G B^T for all tokens, to the waves that own them
       {
         f4 v[4];
@@ -369,6 +367,9 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
       for (int j = 0; j < 4; ++j) m += g4 + j >= col ? v[j] : 0.f;
       m = groups_sum(m);
       if (g4 == 0) f.fd[own] = (first ? 0.f : f.fd[own]) + m;
+      phase();
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) columns(G[q], a.grads, next, q);
       if (wave == 0 && first && turn > 0) finish(h0 + turn / pts - 1);
       block_sync_lds();
     }
@@ -386,7 +387,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
   for (int q = 0; q < NQ; ++q) columns(G[q], a.grads, 0, q);
   block_sync_lds();
   {
-    const int lane = tid & 63;
+    const int lane = fresh_lane();
     // K of columns i = own: accumulator rows are r
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
@@ -399,9 +400,10 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
   }
   for (int turn = 0; turn < turns; ++turn) {
     const bool first = turn % pts == 0;
+    const int next = min(turn + 1, turns - 1);      // the last turn loads itself again: no branch around the loads
     const int h = h0 + turn / pts, pt = turn % pts;
     put(turn);
-    const int lane = fresh(tid) & 63, g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
+    const int lane = fresh_lane(), g4 = 4 * (lane >> 4), col = lane & 15, own = 16 * w + col;
     typename L::Sums& f = s.sums[turn / pts & 1];
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
 #pragma unroll
       for (int k = 0; k < 2; ++k) gp[k] = planes<E, 3>(G[q][2 * k], G[q][2 * k + 1]);
       phase();
-      if (turn + 1 < turns) columns(G[q], a.grads, turn + 1, q);
+      columns(G[q], a.grads, next, q);
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
         Fr<E> xf[2];
@@ -442,7 +444,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
       if (g4 == 0) f.gcol[w][16 * b + col] = (first ? 0.f : f.gcol[w][16 * b + col]) + gc[b];
     }
     phase();
-    if (turn + 1 < turns) fetch(turn + 1);
+    fetch(next);
     // W E and W K of columns i = own: accumulator rows are r
     f4 xacc[4];
     float mcol = 0.f, diag = 0.f, err = 0.f;

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
     };
     auto put = [&](int c) {
       typename L::Buf& u = s.buf[c % NBUF];
-      const int t = fresh(t_), rows = min(C, end - pos - c * C);
+      const int t = w * 64 + fresh_lane(), rows = min(C, end - pos - c * C);
       rx.put(u.X, L::LDP, x + (long)c * C * a.ldx, a.ldx, rows, cols, vx, t);
       rb.put(u.B, L::LDN, B + (long)c * C * a.ldb, a.ldb, rows, a.N, vb, t);
       rc.template put<true>(u.Cm, L::LDM, Cm + (long)c * C * a.ldc, a.ldc, rows, a.N, vc, t);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
     // rows r = 16 w + col, formed as their transposes: accumulator rows are i
     auto scores = [&](int c) {
       typename L::Buf& u = s.buf[c % NBUF];
-      const int lane = fresh(t_) & 63, g4 = 4 * (lane >> 4), col = lane & 15;
+      const int lane = fresh_lane(), g4 = 4 * (lane >> 4), col = lane & 15;
       Fr<E> cf[KN];
 #pragma unroll
       for (int k = 0; k < KN; ++k) cf[k] = step_frag<E>(u.Cm, L::LDM, 16 * w, 32 * k, lane);
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
   for (int c = 0; c < chunks; ++c) {
     const typename L::Buf& u = s.buf[c % NBUF];
     const int rows = min(C, end - pos - c * C);
-    const int lane = fresh(t_) & 63, g4 = 4 * (lane >> 4), col = lane & 15;
+    const int lane = fresh_lane(), g4 = 4 * (lane >> 4), col = lane & 15;
     Fr<E> xt[2];                         // x^T: row p, k = i
 #pragma unroll
     for (int k = 0; k < 2; ++k) xt[k] = col_frag<E>(u.X, L::LDP, 32 * k, 16 * w, lane);

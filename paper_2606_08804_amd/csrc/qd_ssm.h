@@ -125,9 +125,8 @@ template <typename E> __device__ inline int flip(int row, int c) { return sizeof
 
 // Tiles that are read along rows alone ("steps") hold a row's columns in groups
 // of 32 in the order in which a step takes them, the quad 16 blk + 4 g of a group
-// at 8 g + 4 blk: a lane's two quads are then one 16-byte read.  (Two 8-byte
-// reads are joined into one instruction, which takes 16 lanes at a time and so
-// meets half of the banks twice; transpose reads of this order would.)
+// at 8 g + 4 blk: a lane's two quads are then one 16-byte read.  (Transpose reads
+// of this order would meet half of the banks twice.)
 template <typename E> constexpr int steps_ld(int cols) { return cols + 16 / (int)sizeof(E); }
 template <typename E> __device__ constexpr int step_at(int c) {
   return sizeof(E) == 2 ? (c & ~31) + ((c >> 2) & 3) * 8 + ((c >> 4) & 1) * 4 : c;
@@ -145,13 +144,19 @@ __device__ inline Fr<E> step_frag(const E* t, int ld, int row0, int k0, int lane
   return f;
 }
 
-// Operand with i = row0 + l % 16 and k along the row, from k0.
+// Operand with i = row0 + l % 16 and k along the row, from k0.  The two reads
+// are kept from being joined into one instruction, which takes 16 lanes at a
+// time and so meets half of the banks twice (three times the conflicts of the
+// backward's tiles).
 template <typename E>
 __device__ inline Fr<E> row_frag(const E* t, int ld, int row0, int k0, int lane) {
   typedef typename Q4<E>::t q4;
   const int r = lane & 15;
   const E* p = t + (row0 + r) * ld + k0 + flip<E>(r, 4 * (lane >> 4));
-  const q4 a = *(const q4*)p, b = *(const q4*)(p + 16);
+  const q4 a = *(const q4*)p;
+  __builtin_amdgcn_sched_barrier(0);
+  const q4 b = *(const q4*)(p + 16);
+  __builtin_amdgcn_sched_barrier(0);
   Fr<E> f;
   if constexpr (sizeof(E) == 2) {
     f.v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);

@@ -13,18 +13,23 @@ chunk forward and backward, and a module with the gate projections.
     beta = sigmoid(W_beta h); alpha = sigmoid(W_alpha h), passed as its log;
     lambda = sigmoid(W_lambda h + b) with one scalar bias b initialised to
     -0.8 (App. "Query-Feedback Coefficient"); then the recurrence and an output
-    projection.  The short convolutions, output gate and normalisation of the
-    paper's block appear only in its architecture figure (Fig. 1b) and are not
-    part of this layer.
+    projection.  The short convolutions, output normalisation and output gate of
+    the paper's block appear only in its architecture figure (Fig. 1b); they are
+    options (``conv_size``, ``out_norm``, ``out_gate``), off by default.
 
-The projections are ordinary library GEMMs; the q/k normalisation and the
-recurrence are the library's kernels.  There is no CPU path: without the built library every call raises.
+``causal_conv``, ``selective_scan``, ``row_norm``
+    the differentiable forms of the operators of ``mixer``: the short causal
+    convolution, the selective state space scan and the row normalisation.
+
+The projections are ordinary library GEMMs; everything else is the library's
+kernels.  There is no CPU path: without the built library every call raises.
 """
 import math
 
 import torch
 import torch.nn.functional as F
 
+from . import mixer as _mixer
 from . import qdelta as _binding
 
 
@@ -134,6 +139,88 @@ def qdelta_chunk(q, k, v, beta, lam=None, log_alpha=None, initial_state=None, cu
     return QDeltaFunction.apply(q, k, v, beta, lam, log_alpha, initial_state, cu_seqlens)
 
 
+def _dense(d, like):
+    """A gradient as the kernels take it: contiguous, zeros where none came."""
+    return torch.zeros(like.shape, dtype=like.dtype, device=like.device) if d is None else d.contiguous()
+
+
+class CausalConvFunction(torch.autograd.Function):
+    """Autograd wrapper of mixer.conv_fwd and mixer.conv_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, initial_state, cu_seqlens, activation):
+        ctx.set_materialize_grads(False)
+        y, final_state = _mixer.conv_fwd(x, weight, bias, initial_state, cu_seqlens, activation)
+        ctx.activation = activation
+        ctx.save_for_backward(x, weight, bias, initial_state, cu_seqlens)
+        return y, final_state
+
+    @staticmethod
+    def backward(ctx, d_y, d_final_state):
+        x, weight, bias, initial_state, cu_seqlens = ctx.saved_tensors
+        need = initial_state is not None and ctx.needs_input_grad[3]
+        g = _mixer.conv_bwd(x, weight, bias, initial_state, _dense(d_y, x),
+                            None if d_final_state is None else d_final_state.contiguous(), cu_seqlens, ctx.activation,
+                            need_d_initial_state=need)
+        return g["dx"], g["dweight"], g["dbias"], g["d_initial_state"], None, None
+
+
+class SelectiveScanFunction(torch.autograd.Function):
+    """Autograd wrapper of mixer.scan_fwd and mixer.scan_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens, softplus):
+        ctx.set_materialize_grads(False)
+        y, final_state = _mixer.scan_fwd(x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens, softplus)
+        ctx.softplus = softplus
+        ctx.save_for_backward(x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens)
+        return y, final_state
+
+    @staticmethod
+    def backward(ctx, d_y, d_final_state):
+        x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens = ctx.saved_tensors
+        need = initial_state is not None and ctx.needs_input_grad[7]
+        g = _mixer.scan_bwd(x, dt, A, B, C, D, dt_bias, initial_state, _dense(d_y, x),
+                            None if d_final_state is None else d_final_state.contiguous(), cu_seqlens, ctx.softplus,
+                            need_d_initial_state=need)
+        return (g["dx"], g["ddt"], g["dA"], g["dB"], g["dC"], g["dD"], g["ddt_bias"], g["d_initial_state"], None, None)
+
+
+class RowNormFunction(torch.autograd.Function):
+    """Autograd wrapper of mixer.norm_fwd and mixer.norm_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, gate, eps, kind):
+        y, stats = _mixer.norm_fwd(x, weight, bias, gate, eps, kind)
+        ctx.kind = kind
+        ctx.save_for_backward(x, weight, bias, gate, stats)
+        return y
+
+    @staticmethod
+    def backward(ctx, d_y):
+        x, weight, bias, gate, stats = ctx.saved_tensors
+        g = _mixer.norm_bwd(x, weight, bias, gate, stats, d_y.contiguous(), ctx.kind)
+        return g["dx"], g["dweight"], g["dbias"], g["dgate"], None, None
+
+
+def causal_conv(x, weight, bias=None, initial_state=None, cu_seqlens=None, activation=None):
+    """Differentiable short causal convolution: x [B,T,D], weight [D,W], bias
+    [D], state [N,W-1,D] (as mixer.conv_fwd).  Returns (y, final_state)."""
+    return CausalConvFunction.apply(x, weight, bias, initial_state, cu_seqlens, activation)
+
+
+def selective_scan(x, dt, A, B, C, D=None, dt_bias=None, initial_state=None, cu_seqlens=None, softplus=False):
+    """Differentiable selective state space scan: x [B,T,H,P], dt [B,T,H], A [H],
+    B, C [B,T,G,Ns], D, dt_bias [H], state [N,H,P,Ns] (as mixer.scan_fwd).
+    Returns (y, final_state)."""
+    return SelectiveScanFunction.apply(x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens, softplus)
+
+
+def row_norm(x, weight=None, bias=None, gate=None, eps=1e-5, kind="layer"):
+    """Differentiable normalisation of the rows of x [..., D], with a SiLU gate (as mixer.norm_fwd)."""
+    return RowNormFunction.apply(x, weight, bias, gate, eps, kind)
+
+
 class QDeltaLayer(torch.nn.Module):
     """Token mixer of a Q-Delta block: projections, gates, recurrence, output.
 
@@ -142,13 +229,24 @@ class QDeltaLayer(torch.nn.Module):
     q and k L2 norms by the library's row-normalisation kernels."""
 
     def __init__(self, d_model, n_heads, head_dk=128, head_dv=128, use_decay=True, qk_norm=True,
-                 lambda_bias=-0.8, fixed_lambda=None):
+                 lambda_bias=-0.8, fixed_lambda=None, conv_size=0, out_norm=None, out_gate=False):
         """fixed_lambda: None for the learned gate lambda_t = sigmoid(W h + b);
         a number for a constant lambda (the paper's ablations: scalar 0.2, 0.5,
         0.8, and 1.0 for "no gating"), handed to the kernels as a scalar, so no
         lambda tensor is formed or read; 0 gives the gated delta rule.
-        use_decay=False gives alpha == 1 ("no state decay")."""
+        use_decay=False gives alpha == 1 ("no state decay").
+        conv_size: 2 to 4 for a short causal convolution with SiLU over the
+        channels of q, k and v (0: none).  out_norm: "rms" or "layer" for a
+        normalisation of every head's output with a weight of head_dv (and a
+        bias, "layer"); out_gate: that norm's SiLU gate, projected from h."""
         super().__init__()
+        if conv_size not in (0, 2, 3, 4):
+            raise ValueError(f"conv_size must be 0 or 2 to 4, got {conv_size}")
+        if out_norm not in (None, "rms", "layer"):
+            raise ValueError(f"out_norm must be None, 'rms' or 'layer', got {out_norm!r}")
+        if out_gate and out_norm is None:
+            raise ValueError("out_gate is part of the output norm: it needs out_norm")
+        self.conv_size, self.out_norm, self.out_gate = conv_size, out_norm, bool(out_gate)
         self.d_model, self.H, self.dk, self.dv = d_model, n_heads, head_dk, head_dv
         self.use_decay, self.qk_norm = use_decay, qk_norm
         self.fixed_lambda = None if fixed_lambda is None else float(fixed_lambda)
@@ -159,11 +257,26 @@ class QDeltaLayer(torch.nn.Module):
         if self.fixed_lambda is None:
             self.lambda_bias = torch.nn.Parameter(torch.tensor(float(lambda_bias)))
         self.w_out = torch.nn.Linear(n_heads * head_dv, d_model, bias=False)
+        if conv_size:
+            self.conv_weight = torch.nn.Parameter(torch.empty(n_heads * (2 * head_dk + head_dv), conv_size))
+        if out_norm:
+            self.norm_weight = torch.nn.Parameter(torch.empty(head_dv))
+            self.norm_bias = torch.nn.Parameter(torch.empty(head_dv)) if out_norm == "layer" else None
+        if out_gate:
+            self.w_out_gate = torch.nn.Linear(d_model, n_heads * head_dv, bias=False)
         self.reset_parameters()
 
     def reset_parameters(self):
         for lin in (self.w_qkv, self.w_gates, self.w_out):
             torch.nn.init.normal_(lin.weight, std=1.0 / math.sqrt(lin.in_features))
+        if self.conv_size:
+            torch.nn.init.normal_(self.conv_weight, std=1.0 / math.sqrt(self.conv_size))
+        if self.out_norm:
+            torch.nn.init.ones_(self.norm_weight)
+            if self.norm_bias is not None:
+                torch.nn.init.zeros_(self.norm_bias)
+        if self.out_gate:
+            torch.nn.init.normal_(self.w_out_gate.weight, std=1.0 / math.sqrt(self.d_model))
 
     def gates(self, h):
         """beta, lambda, log alpha ([..., H] fp32 or wider; lambda a number
@@ -212,9 +325,16 @@ class QDeltaLayer(torch.nn.Module):
                      or qkv.dtype == torch.float32 and self.dk == 64))
 
     def forward(self, h, initial_state=None, cu_seqlens=None, output_final_state=False):
+        """initial_state and the final state returned: [N,H,dv,dk], with a
+        convolution a pair of that and the convolution's rows [N, conv_size - 1,
+        H (2 dk + dv)]."""
         B, T, _ = h.shape
         H, dk, dv = self.H, self.dk, self.dv
-        qkv = self.w_qkv(h).view(B, T, H, 2 * dk + dv)
+        qkv = self.w_qkv(h)
+        if self.conv_size:
+            initial_state, conv_state = (None, None) if initial_state is None else initial_state
+            qkv, conv_state = causal_conv(qkv, self.conv_weight, None, conv_state, cu_seqlens, "silu")
+        qkv = qkv.view(B, T, H, 2 * dk + dv)
         beta, lam, log_alpha = self._fused_gates(h) if self._can_fuse_gates(h) else self.gates(h)
         gates = (beta.contiguous(), lam.contiguous() if isinstance(lam, torch.Tensor) else lam,
                  None if log_alpha is None else log_alpha.contiguous())
@@ -227,5 +347,10 @@ class QDeltaLayer(torch.nn.Module):
                 k = L2NormFunction.apply(k)
             o, final_state = qdelta_chunk(q.contiguous(), k.contiguous(), v.contiguous(), *gates, initial_state,
                                           cu_seqlens)
+        if self.out_norm:
+            gate = self.w_out_gate(h).view(B, T, H, dv) if self.out_gate else None
+            o = row_norm(o, self.norm_weight, self.norm_bias, gate, kind=self.out_norm)
         y = self.w_out(o.reshape(B, T, H * dv))
+        if self.conv_size:
+            final_state = final_state, conv_state
         return (y, final_state) if output_final_state else y

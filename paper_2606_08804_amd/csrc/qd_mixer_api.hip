@@ -85,7 +85,7 @@ ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd) {
     const size_t slots = (size_t)q.slots(qd::C), tile = (size_t)qd::PT * (Ns <= 64 ? 64 : 128) * 4;
     w.states = take(slots * H * qd::p_tiles(P) * tile);
     w.grads = take(slots * H * qd::p_tiles(P) * tile);
-    w.sums = take(slots * H * 16);
+    w.sums = take(slots * H * 32);
     w.splits = qd::scan_splits(q, H, G);
     if (w.splits > 1) {
       w.partB = take((size_t)w.splits * n_tokens(q) * G * Ns * 4);
@@ -108,7 +108,7 @@ void bind_ws(qd::ScanArgs& a, const ScanWs& w, void* ws) {
   a.grads = at(w.grads);
   a.partB = at(w.partB);
   a.partC = at(w.partC);
-  a.sums = at(w.sums);
+  a.sums = reinterpret_cast<double*>(p + w.sums);
   a.gates = at(w.gates);
 }
 

@@ -226,7 +226,7 @@ struct ScanArgs {
   float *states, *grads;
   int splits;                      // workgroups that share a chunk's heads
   float *partB, *partC;            // [split][tokens][G][N] where splits > 1
-  float* sums;                     // [chunk slot][H][4]: dA, dD, dbias
+  double* sums;                    // [chunk slot][H][4]: dA, dD, dbias
   float* gates;                    // [chunk slot][H] Gates
 };
 

@@ -189,11 +189,15 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
     const bool in = r < rows;
     if (a.softplus) raw *= -expm1f(-step);               // sigmoid of the raw step, from its softplus
     if (in) a.ddt[(t0 + r) * a.H + h] = raw;
-    float sa = in ? step * dl : 0.f, sd = in ? f.err[r] : 0.f, sb = in ? raw : 0.f;
-    sa = groups_sum(sum16(sa));
-    sd = groups_sum(sum16(sd));
-    sb = groups_sum(sum16(sb));
-    if (lane == 0) *(f4*)(a.sums + (slot * a.H + h) * 4) = f4{sa, sd, sb, 0.f};
+    // in 64 bits: these sums cancel over the tokens (dA is 1% of its terms' absolute sum at 16384 tokens)
+    const double sa = wave_incl_scan64(in ? (double)step * (double)dl : 0.0), sd = wave_incl_scan64(in ? (double)f.err[r] : 0.0),
+                 sb = wave_incl_scan64(in ? (double)raw : 0.0);
+    if (lane == 63) {
+      double* out = a.sums + (slot * a.H + h) * 4;
+      out[0] = sa;
+      out[1] = sd;
+      out[2] = sb;
+    }
   };
 
   if (wave < 4) {
@@ -243,9 +247,11 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
       float sr[4] = {};
 #pragma unroll
       for (int q = 0; q < NQ; ++q) {
+        // every second 16 columns with the sign turned, so that the products' one-sided rounding cancels in sr
+        const float sign = NQ > 1 ? (q & 1 ? -1.f : 1.f) : (w & 1 ? -1.f : 1.f);
         Planes<E, 3> sp[2];
 #pragma unroll
-        for (int k = 0; k < 2; ++k) sp[k] = planes<E, 3>(S[q][2 * k], S[q][2 * k + 1]);
+        for (int k = 0; k < 2; ++k) sp[k] = planes<E, 3>(sign * S[q][2 * k], sign * S[q][2 * k + 1]);
         phase();
         columns(S[q], a.states, next, q);
 #pragma unroll
@@ -258,7 +264,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
           f4 u = zero4();
 #pragma unroll
           for (int k = 0; k < 2; ++k) u = mma(sp[k], yf[k], u);
-          u *= er;
+          u *= sign * er;
           accn[q][b] += u;
 #pragma unroll
           for (int j = 0; j < 4; ++j) sr[b] += tof(c[j]) * u[j];
@@ -416,9 +422,11 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
     float gc[4] = {};
 #pragma unroll
     for (int q = 0; q < NQ; ++q) {
+      // as above, for gc
+      const float sign = NQ > 1 ? (q & 1 ? -1.f : 1.f) : (w & 1 ? -1.f : 1.f);
       Planes<E, 3> gp[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) gp[k] = planes<E, 3>(G[q][2 * k], G[q][2 * k + 1]);
+      for (int k = 0; k < 2; ++k) gp[k] = planes<E, 3>(sign * G[q][2 * k], sign * G[q][2 * k + 1]);
       phase();
       columns(G[q], a.grads, next, q);
 #pragma unroll
@@ -431,7 +439,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
         f4 u = zero4();
 #pragma unroll
         for (int k = 0; k < 2; ++k) u = mma(gp[k], xf[k], u);
-        u *= ei;
+        u *= sign * ei;
         accn[q][b] += dt * u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) gc[b] += tof(c[j]) * u[j];
@@ -574,26 +582,30 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_join(ScanArgs a, long n) {
 
 // dA, dD and the bias's gradient of a head: its chunks' sums, in a fixed order.
 __global__ __launch_bounds__(NTHREADS) void k_ssm_heads(ScanArgs a, long slots) {
-  __shared__ f4 red[NTHREADS];
+  __shared__ double red[3][NTHREADS];
   const int h = blockIdx.x, t = threadIdx.x;
-  f4 v = zero4();
+  double v[3] = {};
   for (long k = t; k < slots; k += NTHREADS) {
     int n, len, pos;
     long s0;
     if (a.q.cu && !a.q.locate(k, C, n, s0, len, pos)) continue;
-    v += *(const f4*)(a.sums + (k * a.H + h) * 4);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) v[i] += a.sums[(k * a.H + h) * 4 + i];
   }
-  red[t] = v;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) red[i][t] = v[i];
   __syncthreads();
 #pragma unroll
   for (int off = NTHREADS / 2; off >= 1; off >>= 1) {
-    if (t < off) red[t] += red[t + off];
+    if (t < off)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) red[i][t] += red[i][t + off];
     __syncthreads();
   }
   if (t) return;
-  a.dA[h] = red[0][0];
-  if (a.dD) a.dD[h] = red[0][1];
-  if (a.dbias) a.dbias[h] = red[0][2];
+  a.dA[h] = (float)red[0][0];
+  if (a.dD) a.dD[h] = (float)red[1][0];
+  if (a.dbias) a.dbias[h] = (float)red[2][0];
 }
 
 template <typename E, int NP>

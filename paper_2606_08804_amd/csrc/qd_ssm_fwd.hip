@@ -419,6 +419,12 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
   const E* B = (const E*)(dir ? a.C : a.B) + (s0 + pos) * ldb + (long)grp * a.N;
   const bool vx = vec_rows<E>(x, ldx, cols), vb = vec_rows<E>(B, ldb, a.N);
 
+  // Every second wave holds its rows with the sign turned.  The matrix
+  // instructions' sums lean to one side by a fraction of a last place a step;
+  // that would add up over the chunks and, as <G, S> sums every entry, over P x N
+  // as well.  Rows of both signs cancel it (dA's error 1.0e-6 -> 1.0e-7 of its
+  // largest entry, 4 x 4096 tokens, 64 heads, with the same in the backward).
+  const float sign = w & 1 ? -1.f : 1.f;
   // Without `keep` this is a segment's own contribution, from zero; with it the
   // walk starts from the segment's entry, or the sequence's.
   const float* ends = dir ? a.dSf : a.S0;
@@ -430,7 +436,7 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int p = p0 + 16 * w + g4 + j, nn = 16 * nb + col;
-      S[nb][j] = in && p < a.P && nn < a.N ? in[(long)p * a.N + nn] : 0.f;
+      S[nb][j] = in && p < a.P && nn < a.N ? sign * in[(long)p * a.N + nn] : 0.f;
     }
   double run = 0.0;                      // sum of dt A over the segment
   const int chunks = (end - pos + C - 1) / C;
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
     if (keep) {
       float* out = (dir ? a.grads : a.states) + ((cslot + c) * a.H * pts + hp) * (long)(PT * NP);
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) *(f4*)(out + ((w * NB + nb) * 64 + lane) * 4) = S[nb];
+      for (int nb = 0; nb < NB; ++nb) *(f4*)(out + ((w * NB + nb) * 64 + lane) * 4) = sign * S[nb];
     }
     {
       const int rows = min(C, end - pos - c * C);
@@ -474,7 +480,7 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int at = 32 * k + 16 * i + g4;
-        ws[k][i] = dir ? *(const f4*)(s.g.head + at) : *(const f4*)(s.g.dt + at) * *(const f4*)(s.g.tail + at);
+        ws[k][i] = (dir ? *(const f4*)(s.g.head + at) : *(const f4*)(s.g.dt + at) * *(const f4*)(s.g.tail + at)) * sign;
       }
     }
 #pragma unroll
@@ -510,7 +516,7 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int p = p0 + 16 * w + g4 + j, nn = 16 * nb + col;
-        if (p < a.P && nn < a.N) out[(long)p * a.N + nn] = S[nb][j];
+        if (p < a.P && nn < a.N) out[(long)p * a.N + nn] = sign * S[nb][j];
       }
   if (!whole && !keep && dir == dir0 && p0 == 0 && t == 0) a.decay[slot * a.H + h] = (float)run;
 }

@@ -6,12 +6,19 @@
 //             dw[:, j] = sum_t du_t x_{t - W + 1 + j},  db = sum_t du_t
 //
 // x before a sequence's first token are the rows of its state [W - 1][D], the
-// oldest first, or zero.  A thread owns V channels (16 bytes) and walks a tile
-// of tokens with the last W - 1 rows in registers, so a row is read once and the
-// W - 1 rows before a tile (after it, in the backward, which forms u again)
-// twice.  HBM bounds all of it.  The weight's gradient is summed in registers
-// over a wave's tile, over the workgroup's four tiles in LDS and over the
-// workgroups by a second launch, each in a fixed order.
+// oldest first, or zero.  A thread owns V channels and walks a tile of tokens
+// with the last W - 1 rows in registers, so a row is read once and the W - 1
+// rows before a tile (after it, in the backward, which forms u again) twice.
+// The weight's gradient is summed in registers over a wave's tile, over the
+// workgroup's four tiles in LDS and over the workgroups by a second launch,
+// each in a fixed order.
+//
+// HBM bounds the forward: 4 x 4096 tokens of 6144 channels in bf16, W = 4, take
+// 84 us (403 MB, 4.8 TB/s; pieces of 8 bytes instead of 16: 97 us).  The
+// backward moves 604 MB in 136 us (4.4 TB/s) and runs its vector instructions
+// for 83 us of them; what it needs is loads in flight.  Pieces of 8 bytes keep
+// four of its waves on a SIMD in place of two (190 -> 158 us), and the rows of
+// the next turn are read while this one's are used (158 -> 136 us).
 #include "qd_mixer.h"
 
 namespace qd {
@@ -31,12 +38,24 @@ __device__ inline void load_row(Vec<E, V>& r, const ConvArgs& a, int n, long s, 
 
 template <typename E, int V, int W>
 __device__ inline void load_weights(float (&w)[W][V], float (&b)[V], const ConvArgs& a, int c) {
+  const E* p = (const E*)a.w + (long)c * W;
+  if constexpr (V == 1) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    b[i] = a.b ? tof(((const E*)a.b)[c + i]) : 0.f;
+    for (int j = 0; j < W; ++j) w[j][0] = tof(p[j]);
+  } else {                         // the V channels' taps are W whole pieces
 #pragma unroll
-    for (int j = 0; j < W; ++j) w[j][i] = tof(((const E*)a.w)[(long)(c + i) * W + j]);
+    for (int k = 0; k < W; ++k) {
+      Vec<E, V> t;
+      t.load(p + k * V);
+#pragma unroll
+      for (int i = 0; i < V; ++i) w[(k * V + i) % W][(k * V + i) / W] = t.v[i];
+    }
   }
+  Vec<E, V> t;
+  if (a.b) t.load((const E*)a.b + c);
+  else t.zero();
+#pragma unroll
+  for (int i = 0; i < V; ++i) b[i] = t.v[i];
 }
 
 // Tiles of L tokens by flat thread index, then the final states by further threads.
@@ -98,13 +117,55 @@ __device__ inline float act_grad(float u, float dy, int silu) {
   return dy * (sg * (1.f + u * (1.f - sg)));
 }
 
-// Workgroup: 64 pieces of channels (one a lane) by four successive tiles of BT
-// tokens (one a wave); grid: slots of BSLOT tokens by groups of 64 pieces.
+// Gradient of the initial state, piece k: row i of it is x at position i - (W - 1).
 template <typename E, int V, int W>
-__global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups) {
+__device__ inline void initial_grad(const ConvArgs& a, long k) {
+  const int nv = a.D / V;
+  if (k >= (long)a.q.N * (W - 1) * nv) return;
+  const int c = (int)(k % nv) * V, i = (int)(k / nv % (W - 1)), n = (int)(k / nv / (W - 1));
+  int len;
+  long s;
+  if (!a.q.range(n, s, len)) return;
+  float w[W][V], b[V];
+  load_weights<E, V, W>(w, b, a, c);
+  Vec<E, V> o;
+  if (a.dsf && i >= len) o.load((const E*)a.dsf + ((long)n * (W - 1) + i - len) * a.D + c);   // that row is still in the final state
+  else o.zero();
+  // token t reads the row with tap i - t
+  Vec<E, V> x[2 * W - 2];
+#pragma unroll
+  for (int j = 0; j < 2 * W - 2; ++j) {
+    if (j < W - 1 + min(len, W - 1)) load_row<E, V, W>(x[j], a, n, s, j - (W - 1), c);
+    else x[j].zero();
+  }
+#pragma unroll
+  for (int t = 0; t < W - 1; ++t) {
+    if (t >= len || t > i) continue;
+    Vec<E, V> g;
+    g.load((const E*)a.dy + (s + t) * a.D + c);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      float u = b[e], tap = 0.f;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        u += w[j][e] * x[t + j].v[e];
+        if (j == i - t) tap = w[j][e];
+      }
+      o.v[e] += tap * act_grad(u, g.v[e], a.silu);
+    }
+  }
+  o.store((E*)a.ds0 + ((long)n * (W - 1) + i) * a.D + c);
+}
+
+// Workgroup: 64 pieces of channels (one a lane) by four successive tiles of BT
+// tokens (one a wave); grid: slots of BSLOT tokens by groups of 64 pieces, then
+// the initial states' gradients by flat thread index.
+template <typename E, int V, int W>
+__global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups, long slots) {
   constexpr int U = 4, R = W + 1;
   __shared__ float sum[R][64 * V];
   const long slot = blockIdx.x / cgroups;
+  if (slot >= slots) return initial_grad<E, V, W>(a, (blockIdx.x - slots * cgroups) * NTHREADS + threadIdx.x);
   const int cg = (int)(blockIdx.x - slot * cgroups), lane = threadIdx.x & 63, wave = wave_id(threadIdx.x);
   const int c = (cg * 64 + lane) * V;
   const bool mine = c < a.D;
@@ -127,27 +188,39 @@ __global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups) 
     const E* xp = (const E*)a.x + s * a.ldx + c;
     const E* gp = (const E*)a.dy + s * a.D + c;
     E* dx = (E*)a.dx + s * a.D + c;
-    for (int t0 = pos; t0 < end + W - 1; t0 += U) {
-      Vec<E, V> g[U];
+    // the rows of the next turn are read while this one's are used; rows from `stop` on are read as the last one, and not used
+    typedef typename Vec<E, V>::raw_t raw_t;
+    raw_t xn[U], gn[U];
+    auto fetch = [&](int t0) {
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        g[k].zero();
-        if (t0 + k < stop) {
-          x[W - 1 + k].load(xp + (long)(t0 + k) * a.ldx);
-          g[k].load(gp + (long)(t0 + k) * a.D);
-        } else {
-          x[W - 1 + k].zero();
-        }
+        const int t = min(t0 + k, stop - 1);
+        xn[k] = *(const raw_t*)(xp + (long)t * a.ldx);
+        gn[k] = *(const raw_t*)(gp + (long)t * a.D);
       }
+    };
+    fetch(pos);
+    for (int t0 = pos; t0 < end + W - 1; t0 += U) {
+      raw_t xr[U], gr[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        xr[k] = xn[k];
+        gr[k] = gn[k];
+      }
+      fetch(t0 + U);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < U; ++k) {
         const int t = t0 + k;                            // du_t, then the row t - (W - 1) of dx
+        Vec<E, V> g;
+        g.take(gr[k]);
+        x[W - 1 + k].take(xr[k]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float u = b[e];
 #pragma unroll
           for (int j = 0; j < W; ++j) u += w[j][e] * x[k + j].v[e];
-          const float d = t < stop ? act_grad(u, g[k].v[e], a.silu) : 0.f;
+          const float d = t < stop ? act_grad(u, g.v[e], a.silu) : 0.f;
           du[W - 1 + k][e] = d;
           if (t < end) {
 #pragma unroll
@@ -186,47 +259,6 @@ __global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups) 
     const int r = k / (64 * V), d = cg * 64 * V + k % (64 * V);
     if (d < a.D) a.part[(slot * R + r) * a.D + d] = sum[r][k % (64 * V)];
   }
-}
-
-// Gradient of the initial state: row i of it is x at position i - (W - 1).
-template <typename E, int V, int W>
-__global__ __launch_bounds__(NTHREADS) void k_conv_ds0(ConvArgs a) {
-  const int nv = a.D / V;
-  const long k = (long)blockIdx.x * NTHREADS + threadIdx.x;
-  if (k >= (long)a.q.N * (W - 1) * nv) return;
-  const int c = (int)(k % nv) * V, i = (int)(k / nv % (W - 1)), n = (int)(k / nv / (W - 1));
-  int len;
-  long s;
-  if (!a.q.range(n, s, len)) return;
-  float w[W][V], b[V];
-  load_weights<E, V, W>(w, b, a, c);
-  Vec<E, V> o;
-  if (a.dsf && i >= len) o.load((const E*)a.dsf + ((long)n * (W - 1) + i - len) * a.D + c);   // that row is still in the final state
-  else o.zero();
-  // token t reads the row with tap i - t
-  Vec<E, V> x[2 * W - 2];
-#pragma unroll
-  for (int j = 0; j < 2 * W - 2; ++j) {
-    if (j < W - 1 + min(len, W - 1)) load_row<E, V, W>(x[j], a, n, s, j - (W - 1), c);
-    else x[j].zero();
-  }
-#pragma unroll
-  for (int t = 0; t < W - 1; ++t) {
-    if (t >= len || t > i) continue;
-    Vec<E, V> g;
-    g.load((const E*)a.dy + (s + t) * a.D + c);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      float u = b[e], tap = 0.f;
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        u += w[j][e] * x[t + j].v[e];
-        if (j == i - t) tap = w[j][e];
-      }
-      o.v[e] += tap * act_grad(u, g.v[e], a.silu);
-    }
-  }
-  o.store((E*)a.ds0 + ((long)n * (W - 1) + i) * a.D + c);
 }
 
 // One token: a thread owns V channels of one sequence and reads all of its rows before it writes.
@@ -271,11 +303,10 @@ hipError_t fwd(const ConvArgs& a, hipStream_t st) {
 template <typename E, int V, int W>
 hipError_t bwd(const ConvArgs& a, hipStream_t st) {
   const int cgroups = (a.D / V + 63) / 64;
-  const long slots = conv_bwd_slots(a.q);
-  if (slots > 0) hipLaunchKernelGGL((k_conv_bwd<E, V, W>), dim3((unsigned)(slots * cgroups)), dim3(NTHREADS), 0, st, a, cgroups);
-  const long states = a.ds0 ? (long)a.q.N * (W - 1) * (a.D / V) : 0;
-  if (states > 0)
-    hipLaunchKernelGGL((k_conv_ds0<E, V, W>), dim3((unsigned)((states + NTHREADS - 1) / NTHREADS)), dim3(NTHREADS), 0, st, a);
+  const long slots = conv_bwd_slots(a.q), states = a.ds0 ? (long)a.q.N * (W - 1) * (a.D / V) : 0;
+  const long blocks = slots * cgroups + (states + NTHREADS - 1) / NTHREADS;
+  if (blocks > 0)
+    hipLaunchKernelGGL((k_conv_bwd<E, V, W>), dim3((unsigned)blocks), dim3(NTHREADS), 0, st, a, cgroups, slots);
   return hipGetLastError();
 }
 
@@ -289,24 +320,25 @@ hipError_t step(const ConvArgs& a, hipStream_t st) {
 bool whole(const ConvArgs& a, int esz) {
   const int v = 16 / esz;
   uintptr_t p = 0;
-  for (const void* q : {a.x, a.s0, (const void*)a.y, (const void*)a.sf, a.dy, a.dsf, (const void*)a.dx, (const void*)a.ds0})
+  for (const void* q : {a.x, a.w, a.b, a.s0, (const void*)a.y, (const void*)a.sf, a.dy, a.dsf, (const void*)a.dx, (const void*)a.ds0})
     p |= (uintptr_t)q;
   return a.D % v == 0 && a.ldx % v == 0 && (p & 15) == 0;
 }
 
-#define QD_CONV(FN)                                                                                                    \
+// VB: channels of a thread for bf16 (see above); for fp32, 16 bytes of them.
+#define QD_CONV(FN, VB)                                                                                                \
   template <typename E, int V>                                                                                         \
   hipError_t FN##_w(const ConvArgs& a, hipStream_t st) {                                                               \
     return a.W == 2 ? FN<E, V, 2>(a, st) : a.W == 3 ? FN<E, V, 3>(a, st) : a.W == 4 ? FN<E, V, 4>(a, st)               \
                                                                                     : hipErrorInvalidValue;            \
   }                                                                                                                    \
   hipError_t FN##_e(const ConvArgs& a, int dtype, hipStream_t st) {                                                    \
-    if (dtype == 1) return whole(a, 2) ? FN##_w<__bf16, 8>(a, st) : FN##_w<__bf16, 1>(a, st);                          \
+    if (dtype == 1) return whole(a, 2) ? FN##_w<__bf16, VB>(a, st) : FN##_w<__bf16, 1>(a, st);                         \
     return whole(a, 4) ? FN##_w<float, 4>(a, st) : FN##_w<float, 1>(a, st);                                            \
   }
-QD_CONV(fwd)
-QD_CONV(bwd)
-QD_CONV(step)
+QD_CONV(fwd, 8)
+QD_CONV(bwd, 4)
+QD_CONV(step, 8)
 #undef QD_CONV
 
 }  // namespace

@@ -2,38 +2,34 @@
 // normalisation, state space scan): row vectors, sequence tiles, column sums.
 #pragma once
 
+#include <type_traits>
+
 #include "qd_common.h"
 
 namespace qd {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
-// V consecutive activations of a row, widened to fp32.  V is 16 bytes' worth,
-// or 1 where rows are not whole aligned 16-byte pieces.
+// V consecutive activations of a row, widened to fp32.  V is 16 or 8 bytes'
+// worth, or 1 where rows are not whole aligned 16-byte pieces.
 template <typename E, int V>
 struct Vec {
+  static_assert(V == 1 || V * sizeof(E) == 16 || V * sizeof(E) == 8, "pieces of 16 or 8 bytes");
+  typedef unsigned int words __attribute__((ext_vector_type(V * sizeof(E) == 16 ? 4 : 2)));
+  typedef std::conditional_t<V == 1, E, words> raw_t;    // as it lies in memory
   float v[V];
-  __device__ inline void load(const E* p) {
-    if constexpr (V == 1) {
-      v[0] = tof(*p);
-    } else {
-      static_assert(V * sizeof(E) == 16, "16-byte pieces");
-      const u32x4 raw = *(const u32x4*)p;
-      const E* e = (const E*)&raw;
+  __device__ inline void take(const raw_t& raw) {
+    const E* e = (const E*)&raw;
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = tof(e[i]);
-    }
+    for (int i = 0; i < V; ++i) v[i] = tof(e[i]);
   }
+  __device__ inline void load(const E* p) { take(*(const raw_t*)p); }
   __device__ inline void store(E* p) const {
-    if constexpr (V == 1) {
-      *p = fromf<E>(v[0]);
-    } else {
-      u32x4 raw;
-      E* e = (E*)&raw;
+    raw_t raw;
+    E* e = (E*)&raw;
 #pragma unroll
-      for (int i = 0; i < V; ++i) e[i] = fromf<E>(v[i]);
-      *(u32x4*)p = raw;
-    }
+    for (int i = 0; i < V; ++i) e[i] = fromf<E>(v[i]);
+    *(raw_t*)p = raw;
   }
   __device__ inline void zero() {
 #pragma unroll

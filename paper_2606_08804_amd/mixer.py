@@ -21,6 +21,7 @@ are contiguous.  All tensors of a call live on one device, whose current
 stream the call runs on.  Differentiable forms are in ``layer``.
 """
 import ctypes
+import math
 
 import torch
 
@@ -77,8 +78,9 @@ def _call(fn, device, *args):
 
 
 def _one_device(first, *others):
+    index = first.get_device()
     for t in others:
-        if t is not None and t.device != first.device:
+        if t is not None and t.get_device() != index:
             raise ValueError(f"tensors on {first.device} and {t.device}: all of a call's live on one device")
     return first.device
 
@@ -86,18 +88,18 @@ def _one_device(first, *others):
 def _rows(t, name, dtype, lead, size):
     """Elements from one row of t [*lead, *size] to the next; t may be a view whose rows are evenly spaced and whose
     last len(size) dimensions are contiguous within a row."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == lead + size:
+        return math.prod(size)
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} is required")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != tuple(lead) + tuple(size):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(lead) + tuple(size)}")
-    width = 1
-    for d in size:
-        width *= d
-    if t.numel() == 0 or t.is_contiguous():
+    if t.shape != lead + size:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {lead + size}")
+    width = math.prod(size)
+    if t.numel() == 0:
         return width
     k, inner, strides = len(lead), 1, t.stride()
     for i in range(t.dim() - 1, k - 1, -1):
@@ -223,10 +225,7 @@ def _norm_args(x, weight, bias, gate, kind):
     _opt(weight, "weight", x.dtype, (D,))
     _opt(bias, "bias", x.dtype, (D,))
     ldg = D if gate is None else _rows(gate, "gate", x.dtype, lead, (D,))
-    rows = 1
-    for d in lead:
-        rows *= d
-    return lead, rows, D, ldx, ldg
+    return lead, math.prod(lead), D, ldx, ldg
 
 
 def norm_fwd(x, weight=None, bias=None, gate=None, eps=1e-5, kind="layer"):

@@ -290,9 +290,12 @@ template <typename E, int V, int W>
 hipError_t fwd(const ConvArgs& a, hipStream_t st) {
   const int nv = a.D / V;
   const long tokens = a.q.cu ? a.q.T : (long)a.q.N * a.q.T;
-  // Tiles of 32 tokens once they give every CU eight waves, else of 8: short
-  // prompts need the threads more than they save rows read twice.
-  const int L = tokens / 32 * nv >= 1 << 17 ? 32 : 8;
+  // The longest tiles that give every CU eight waves: few rows are read twice
+  // then, but short prompts need the threads more (6144 channels, forward and
+  // backward with tiles of 8, 16, 32, 64: 4 x 4096 tokens 241, 229, 224, 219 us,
+  // 4096 tokens 59, 56, 58, 70, 1024 tokens 35, 37, 44, 59).
+  int L = 64;
+  while (L > 8 && tokens / L * nv < 1 << 17) L /= 2;
   const long tiles = a.q.slots(L) * nv, states = a.sf ? (long)a.q.N * (W - 1) * nv : 0;
   if (tiles + states == 0) return hipSuccess;
   const dim3 grid((unsigned)((tiles + states + NTHREADS - 1) / NTHREADS));

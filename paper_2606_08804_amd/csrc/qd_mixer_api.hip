@@ -64,7 +64,7 @@ struct ScanWs {
   int seg = 0, splits = 1;
   size_t entry[2] = {0, 0}, total[2] = {0, 0}, decay = 0, states = 0, grads = 0, partB = 0, partC = 0, sums = 0, gates = 0, bytes = 0;
 };
-ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd) {
+ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd, bool f32) {
   ScanWs w;
   auto take = [&](size_t n) {
     const size_t at = w.bytes;
@@ -72,7 +72,7 @@ ScanWs scan_ws(const qd::Seqs& q, int H, int G, int P, int Ns, bool bwd) {
     return at;
   };
   w.gates = take((size_t)q.slots(qd::C) * H * qd::GATES * 4);
-  w.seg = qd::scan_segment(q, H, P, bwd ? 2 : 1);
+  w.seg = qd::scan_segment(q, H, P, bwd ? 2 : 1, f32);
   if (w.seg) {
     const size_t heads = (size_t)q.slots(w.seg) * H;
     for (int d = 0; d < (bwd ? 2 : 1); ++d) {
@@ -143,7 +143,7 @@ size_t qdelta_scan_workspace_bytes(int32_t N, int32_t T, int32_t packed, int32_t
   if (check_seqs(N, T, packed ? &any : nullptr, q) ||
       check_scan(q, H, G, P, Ns, QDELTA_F32, INT64_MAX, INT64_MAX, INT64_MAX))
     return 0;
-  return scan_ws(q, H, G, P, Ns, is_bwd != 0).bytes;
+  return scan_ws(q, H, G, P, Ns, is_bwd != 0, true).bytes;   // fp32 has the shorter segments: at least as many of them
 }
 
 int qdelta_scan_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, int32_t G, int32_t P, int32_t Ns,
@@ -157,7 +157,7 @@ int qdelta_scan_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, 
   if (rc) return rc;
   if (n_tokens(a.q) > 0 && !ok_ptr(y, elem_size(dtype))) return QDELTA_EINVAL;
   if (!ok_opt(final_state, 4)) return QDELTA_EINVAL;
-  const ScanWs w = scan_ws(a.q, H, G, P, Ns, false);
+  const ScanWs w = scan_ws(a.q, H, G, P, Ns, false, dtype == QDELTA_F32);
   if (w.bytes > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
   if (ws_bytes < w.bytes) return QDELTA_ENOWORKSPACE;
   if (N == 0) return QDELTA_OK;
@@ -185,7 +185,7 @@ int qdelta_scan_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, 
   }
   if (!ok_ptr(dA, 4) || !ok_opt(dD, 4) || !ok_opt(ddt_bias, 4) || !ok_opt(d_initial_state, 4) || !ok_opt(d_final_state, 4))
     return QDELTA_EINVAL;
-  const ScanWs w = scan_ws(a.q, H, G, P, Ns, true);
+  const ScanWs w = scan_ws(a.q, H, G, P, Ns, true, dtype == QDELTA_F32);
   if (w.bytes > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
   if (ws_bytes < w.bytes) return QDELTA_ENOWORKSPACE;
   a.dy = dy; a.dSf = d_final_state;

@@ -272,7 +272,9 @@ hipError_t bwd(const RowNormArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Lanes a row by its pieces: 16 lanes of one, a wave of one or four, else the workgroup.
+// Lanes a row by its pieces: 16 lanes of one, a wave of one or four, else the
+// workgroup (rows of 256 pieces by the workgroup, one each: backward 56 us
+// instead of 49, its sums meet barriers).
 #define QD_ROWNORM(FN)                                             \
   const int nv = (a.D + V - 1) / V;                                \
   if (nv <= 16) return FN<E, V, 16, 1>(a, st);                     \
@@ -303,10 +305,12 @@ bool whole(const RowNormArgs& a, int esz) {
 }  // namespace
 
 // Workgroups of the backward: enough to fill the chip, few enough that their
-// partial rows (2 D floats each) stay small beside the tensors.
+// partial rows (2 D floats each) stay small beside the tensors (forward and
+// backward with 256, 512 and 1024: 16384 x 2048 in bf16 81, 78, 88 us; 262144
+// gated rows of 128 with 1024 and 2048: 93 and 99 us).
 int norm_bwd_blocks(long rows, int D) {
   long n = (1L << 20) / D;
-  n = n < 256 ? 256 : n > 2048 ? 2048 : n;
+  n = n < 256 ? 256 : n > 1024 ? 1024 : n;
   return (int)(rows < n ? (rows < 1 ? 1 : rows) : n);
 }
 

@@ -394,7 +394,7 @@ hipError_t launch_scan_walks(const ScanArgs& a, int dtype, int dirs, bool chunks
 // From the segments' totals and decays to their entries (direction as above), and the ends.
 hipError_t launch_scan_compose(const ScanArgs& a, int dirs, hipStream_t st);
 // Tokens of a segment for a walk of `dirs` directions; 0: whole sequences.
-int scan_segment(const Seqs& q, int H, int P, int dirs);
+int scan_segment(const Seqs& q, int H, int P, int dirs, bool f32);
 int scan_splits(const Seqs& q, int H, int G);
 
 }  // namespace qd

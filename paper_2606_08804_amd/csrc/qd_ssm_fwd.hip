@@ -618,16 +618,22 @@ hipError_t launch_scan_compose(const ScanArgs& a, int dirs, hipStream_t st) {
   return hipGetLastError();
 }
 
-// A walk takes about 2 us a chunk whatever runs beside it, up to two
-// workgroups a CU; so sequences are cut until that many run, into no less than
-// four chunks (a segment costs a second walk without outputs, and its state).
-int scan_segment(const Seqs& q, int H, int P, int dirs) {
+// Walks are serial over their chunks, so a call of few heads is cut into
+// segments until two of them run on every CU (16 heads of 128 x 128, bf16
+// prompts, segments for one, two and four a CU: 65536 tokens 604, 560, 577 us,
+// 16384 tokens 164, 159, 181; uncut 3190 and 745).  A segment costs a second
+// walk without outputs and its state, so it has eight chunks at least in bf16
+// (4096 tokens, four and eight chunks: 71 and 64 us) and two in fp32, where a
+// chunk takes longer (3001 packed tokens of 8 heads of 64 x 64, forward and
+// backward, two, four and eight: 136, 157 and 194 us).
+int scan_segment(const Seqs& q, int H, int P, int dirs, bool f32) {
   const long tokens = q.cu ? q.T : (long)q.N * q.T, want = 2L * device_cu_count();
   const long units = (long)q.N * H * p_tiles(P) * dirs;
   if (units <= 0 || units >= want / 2) return 0;
   const long slots = want / ((long)H * p_tiles(P) * dirs);       // segments to have in all
   long chunks = (tokens / (slots > 0 ? slots : 1) + C - 1) / C;
-  if (chunks < 4) chunks = 4;
+  const long least = f32 ? 2 : 8;
+  if (chunks < least) chunks = least;
   return q.T <= chunks * C ? 0 : (int)(chunks * C);
 }
 

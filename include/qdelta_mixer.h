@@ -11,9 +11,14 @@
  *
  * Sequences: cu_seqlens NULL is a dense batch of N sequences of T tokens
  * (token (n, t) is row n T + t); else N sequences are packed into T tokens as
- * in qdelta.h (int32[N + 1] on the device, cu[0] = 0, cu[N] = T).  A malformed
- * cu_seqlens leaves the outputs of the sequences concerned unspecified; memory
- * is never accessed out of bounds. */
+ * in qdelta.h (int32[N + 1] on the device, cu[0] = 0, cu[N] = T).  Where cu[N]
+ * < T the tokens from cu[N] on are not read into any result and their rows of
+ * the outputs stay as they are.  A malformed cu_seqlens leaves the outputs of
+ * the sequences concerned unspecified; memory is never accessed out of bounds.
+ *
+ * Sizes: a call has less than 2^31 tokens (N T where dense), and one whose
+ * launches would need 2^32 threads or more is QDELTA_EUNSUPPORTED (for the scan
+ * about 2^23 heads over all sequences, or 2^31 over all tokens). */
 #ifndef QDELTA_MIXER_H
 #define QDELTA_MIXER_H
 

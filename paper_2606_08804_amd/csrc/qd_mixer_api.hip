@@ -28,14 +28,16 @@ int check_seqs(int32_t N, int32_t T, const int32_t* cu, qd::Seqs& q) {
 
 int64_t n_tokens(const qd::Seqs& q) { return q.cu ? (int64_t)q.T : (int64_t)q.N * q.T; }
 
-// Launches of 256 threads, one per piece, stay within the grid's 32 bits.
-constexpr int64_t kMaxThreads = (int64_t(1) << 31) * 256 - 256;
+// A launch has less than 2^32 threads.
+constexpr int64_t kMaxThreads = int64_t(1) << 32;
 
 int check_conv(const qd::Seqs& q, int32_t D, int32_t W, int32_t dtype, int64_t ldx) {
   if (D <= 0 || W <= 0 || ldx < D) return QDELTA_EINVAL;
   if (dtype != QDELTA_F32 && dtype != QDELTA_BF16) return QDELTA_EINVAL;
   if (W < 2 || W > 4) return QDELTA_EUNSUPPORTED;
-  if ((n_tokens(q) + (int64_t)q.N * 4) * D >= kMaxThreads) return QDELTA_EUNSUPPORTED;
+  // threads of the forward and the step in single channels; tiles shorter than
+  // 64 tokens are taken up to 2^17 threads of tiles of 64
+  if ((q.slots(64) + 3 * (int64_t)q.N) * D + (int64_t(1) << 20) >= kMaxThreads) return QDELTA_EUNSUPPORTED;
   return QDELTA_OK;
 }
 
@@ -52,8 +54,12 @@ int check_scan(const qd::Seqs& q, int32_t H, int32_t G, int32_t P, int32_t Ns, i
   if (dtype != QDELTA_F32 && dtype != QDELTA_BF16) return QDELTA_EINVAL;
   if (P > 256 || Ns > 128) return QDELTA_EUNSUPPORTED;
   if (ldx < (int64_t)H * P || ldb < (int64_t)G * Ns || ldc < (int64_t)G * Ns) return QDELTA_EINVAL;
-  // work items and (token, head) numbers stay within the grid's 32 bits
+  // (token, head) numbers stay within 32 bits, and launches of 512 threads a
+  // walk or (chunk, group) and of 256 for 16 heads of a chunk within theirs
   if ((n_tokens(q) + 64 * (int64_t)q.N) * H >= (int64_t(1) << 31)) return QDELTA_EUNSUPPORTED;
+  const int64_t walks = (int64_t)(q.N > 0 ? q.N : 1) * H * qd::p_tiles(P), chunks = q.slots(qd::C);
+  if ((walks + 8) * 512 >= kMaxThreads || (chunks * G + 8) * 512 >= kMaxThreads || chunks * ((H + 15) / 16) * 256 >= kMaxThreads)
+    return QDELTA_EUNSUPPORTED;
   return QDELTA_OK;
 }
 
@@ -143,7 +149,7 @@ size_t qdelta_scan_workspace_bytes(int32_t N, int32_t T, int32_t packed, int32_t
   if (check_seqs(N, T, packed ? &any : nullptr, q) ||
       check_scan(q, H, G, P, Ns, QDELTA_F32, INT64_MAX, INT64_MAX, INT64_MAX))
     return 0;
-  return scan_ws(q, H, G, P, Ns, is_bwd != 0, true).bytes;   // fp32 has the shorter segments: at least as many of them
+  return scan_ws(q, H, G, P, Ns, is_bwd != 0, true).bytes;   // of either type: fp32 has the shorter segments
 }
 
 int qdelta_scan_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, int32_t G, int32_t P, int32_t Ns,
@@ -157,9 +163,10 @@ int qdelta_scan_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, 
   if (rc) return rc;
   if (n_tokens(a.q) > 0 && !ok_ptr(y, elem_size(dtype))) return QDELTA_EINVAL;
   if (!ok_opt(final_state, 4)) return QDELTA_EINVAL;
+  const size_t need = scan_ws(a.q, H, G, P, Ns, false, true).bytes;
+  if (need > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
+  if (ws_bytes < need) return QDELTA_ENOWORKSPACE;
   const ScanWs w = scan_ws(a.q, H, G, P, Ns, false, dtype == QDELTA_F32);
-  if (w.bytes > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
-  if (ws_bytes < w.bytes) return QDELTA_ENOWORKSPACE;
   if (N == 0) return QDELTA_OK;
   a.y = y;
   a.Sf = final_state;
@@ -185,9 +192,10 @@ int qdelta_scan_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, 
   }
   if (!ok_ptr(dA, 4) || !ok_opt(dD, 4) || !ok_opt(ddt_bias, 4) || !ok_opt(d_initial_state, 4) || !ok_opt(d_final_state, 4))
     return QDELTA_EINVAL;
+  const size_t need = scan_ws(a.q, H, G, P, Ns, true, true).bytes;
+  if (need > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
+  if (ws_bytes < need) return QDELTA_ENOWORKSPACE;
   const ScanWs w = scan_ws(a.q, H, G, P, Ns, true, dtype == QDELTA_F32);
-  if (w.bytes > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
-  if (ws_bytes < w.bytes) return QDELTA_ENOWORKSPACE;
   a.dy = dy; a.dSf = d_final_state;
   a.dx = dx; a.ddt = ddt; a.dA = dA; a.dB = dB; a.dC = dC; a.dD = dD; a.dbias = ddt_bias; a.dS0 = d_initial_state;
   bind_ws(a, w, ws);
@@ -202,6 +210,7 @@ int qdelta_scan_step(int32_t N, int32_t H, int32_t G, int32_t P, int32_t Ns, int
   const int rc = scan_args(a, N, 1, nullptr, H, G, P, Ns, dtype, softplus, x, ldx, dt, A, B, ldb, C, ldc, D, dt_bias, state);
   if (rc) return rc;
   if (N > 0 && !(ok_ptr(state, 4) && ok_ptr(state_out, 4) && ok_ptr(y, elem_size(dtype)))) return QDELTA_EINVAL;
+  if ((int64_t)N * H * ((P + 15) / 16) * 256 >= kMaxThreads) return QDELTA_EUNSUPPORTED;
   a.y = y;
   a.Sf = state_out;
   return status(qd::launch_scan_step(a, dtype, stream));
@@ -249,7 +258,7 @@ int qdelta_conv_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t D, 
   const size_t need = (size_t)qd::conv_bwd_slots(a.q) * (W + 1) * D * sizeof(float);
   if (need > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
   if (ws_bytes < need) return QDELTA_ENOWORKSPACE;
-  if ((int64_t)qd::conv_bwd_slots(a.q) * D >= (int64_t(1) << 31)) return QDELTA_EUNSUPPORTED;
+  if ((int64_t)qd::conv_bwd_slots(a.q) * (D + 63) * 4 + 3 * (int64_t)N * D + 256 >= kMaxThreads) return QDELTA_EUNSUPPORTED;
   a.D = D; a.W = W; a.silu = silu != 0; a.ldx = ldx;
   a.x = x; a.w = weight; a.b = bias; a.s0 = initial_state;
   a.dy = dy; a.dsf = d_final_state;

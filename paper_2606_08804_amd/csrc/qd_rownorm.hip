@@ -43,9 +43,9 @@ template <typename E, int V, int LANES, int K>
 __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   __shared__ float red[4];
   constexpr int RPB = NTHREADS / LANES;
-  const long row = (long)blockIdx.x * RPB + threadIdx.x / LANES;
+  const long row = ((long)blockIdx.y * gridDim.x + blockIdx.x) * RPB + threadIdx.x / LANES;
   const int lane = threadIdx.x % LANES;
-  if (row >= a.rows) return;               // LANES == 256: never; else whole lane groups leave together
+  if (row >= a.rows) return;               // whole lane groups leave together, a workgroup that is one as a whole
   const E* x = (const E*)a.x + row * a.ldx;
   Vec<E, V> v[K];
   float s = 0.f;
@@ -259,7 +259,9 @@ __global__ __launch_bounds__(CS_COLS* CS_ROWS) void k_colsum(const float* __rest
 template <typename E, int V, int LANES, int K>
 hipError_t fwd(const RowNormArgs& a, hipStream_t st) {
   constexpr int RPB = NTHREADS / LANES;
-  hipLaunchKernelGGL((k_norm_fwd<E, V, LANES, K>), dim3((unsigned)((a.rows + RPB - 1) / RPB)), dim3(NTHREADS), 0, st, a);
+  const long blocks = (a.rows + RPB - 1) / RPB, wide = 1L << 23;     // a launch's dimension has less than 2^32 threads
+  const dim3 grid((unsigned)(blocks < wide ? blocks : wide), (unsigned)((blocks + wide - 1) / wide));
+  hipLaunchKernelGGL((k_norm_fwd<E, V, LANES, K>), grid, dim3(NTHREADS), 0, st, a);
   return hipGetLastError();
 }
 

@@ -573,7 +573,9 @@ template <typename E>
 __global__ __launch_bounds__(NTHREADS) void k_ssm_join(ScanArgs a, long n) {
   const float* part = blockIdx.y ? a.partB : a.partC;
   E* out = (E*)(blockIdx.y ? a.dB : a.dC);
-  for (long i = (long)blockIdx.x * NTHREADS + threadIdx.x; i < n; i += (long)gridDim.x * NTHREADS) {
+  long n_end = n;
+  if (a.q.cu) n_end = min(n_end, (long)max(a.q.cu[a.q.N], 0) * a.G * a.N);   // rows from the last sequence's end on stay as they are
+  for (long i = (long)blockIdx.x * NTHREADS + threadIdx.x; i < n_end; i += (long)gridDim.x * NTHREADS) {
     float v = part[i];
     for (int k = 1; k < a.splits; ++k) v += part[k * n + i];
     out[i] = fromf<E>(v);

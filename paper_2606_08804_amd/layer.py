@@ -28,6 +28,7 @@ import math
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 from . import mixer as _mixer
 from . import qdelta as _binding
@@ -156,6 +157,7 @@ class CausalConvFunction(torch.autograd.Function):
         return y, final_state
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_y, d_final_state):
         x, weight, bias, initial_state, cu_seqlens = ctx.saved_tensors
         need = initial_state is not None and ctx.needs_input_grad[3]
@@ -177,6 +179,7 @@ class SelectiveScanFunction(torch.autograd.Function):
         return y, final_state
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_y, d_final_state):
         x, dt, A, B, C, D, dt_bias, initial_state, cu_seqlens = ctx.saved_tensors
         need = initial_state is not None and ctx.needs_input_grad[7]
@@ -197,6 +200,7 @@ class RowNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_y):
         x, weight, bias, gate, stats = ctx.saved_tensors
         g = _mixer.norm_bwd(x, weight, bias, gate, stats, d_y.contiguous(), ctx.kind)

@@ -17,7 +17,9 @@ scan_step(x, dt, A, B, C, state, D=None, dt_bias=None, softplus=False) -> y   (o
 
 x, B and C of the convolution and the scan and x and gate of the norm may be
 views with evenly spaced rows (slices of a fused projection); other tensors
-are contiguous.  All tensors of a call live on one device, whose current
+are contiguous.  cu_seqlens ends at T: padding behind the last sequence is a
+sequence of its own (rows of new outputs past cu_seqlens[-1] are not written).
+All tensors of a call live on one device, whose current
 stream the call runs on.  Differentiable forms are in ``layer``.
 """
 import ctypes

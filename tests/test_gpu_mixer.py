@@ -292,3 +292,52 @@ def test_scan_decay_that_wipes_the_state():
     gr, gm = (ref.scan_grads(*args, f64(dy[0]), f64(dsf[0]), mag=m) for m in (False, True))
     for k in ("dx", "dB", "dC", "ddt"):
         close(g[k][0], gr[k], gm[k], k)
+
+
+# --------------------------------------------------------------------- padding behind the last sequence; many rows
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_behind_the_last_sequence(monkeypatch, dtype):
+    """A packed batch in a longer buffer: its results are those without the padding, bit for bit (the padding crosses no
+    multiple of 128 tokens, so the tiles are the same), and the padding's rows of the outputs stay as they are."""
+    lens, pad = [70, 1, 0, 130], 37
+    T, H, G, P, N = sum(lens), 8, 2, 48, 24
+    _, cu = sequences(lens, True)
+    r = rand(77, dtype)
+    nan = lambda t: torch.cat([t, torch.full_like(t[:, :1], float("nan")).expand(-1, pad, *t.shape[2:])], 1)     # noqa: E731
+    scan = dict(x=r(1, T, H, P), dt=r(1, T, H, t=torch.float32), B=r(1, T, G, N), C=r(1, T, G, N), dy=r(1, T, H, P))
+    fixed = dict(A=-r(H, t=torch.float32).abs() - 0.1, D=r(H, t=torch.float32), dt_bias=r(H, t=torch.float32) - 2)
+    conv = dict(x=r(1, T, 72), dy=r(1, T, 72))
+    w, b = r(72, 4), r(72)
+    empty = torch.empty
+
+    def sevens(*shape, **kw):
+        t = empty(*shape, **kw)
+        return t.fill_(7) if t.dtype != torch.uint8 else t
+
+    def run(s, c):
+        y, S = mixer.scan_fwd(s["x"], s["dt"], fixed["A"], s["B"], s["C"], fixed["D"], fixed["dt_bias"], None, cu, True)
+        g = mixer.scan_bwd(s["x"], s["dt"], fixed["A"], s["B"], s["C"], fixed["D"], fixed["dt_bias"], None, s["dy"],
+                           cu_seqlens=cu, softplus=True)
+        z, rows = mixer.conv_fwd(c["x"], w, b, None, cu, "silu")
+        h = mixer.conv_bwd(c["x"], w, b, None, c["dy"], cu_seqlens=cu, activation="silu")
+        tokens = [y, g["dx"], g["dB"], g["dC"], g["ddt"], z, h["dx"]]
+        return tokens, [S, g["dA"], g["dD"], g["ddt_bias"], g["d_initial_state"], rows, h["dweight"], h["dbias"],
+                        h["d_initial_state"]]
+    want, want_rest = run(scan, conv)
+    padded = [{k: nan(v) for k, v in d.items()} for d in (scan, conv)]
+    monkeypatch.setattr(torch, "empty", sevens)
+    got, got_rest = run(*padded)
+    for a, e in zip(got, want):
+        assert torch.equal(a[:, :T], e) and (a[:, T:] == 7).all()
+    for a, e in zip(got_rest, want_rest):
+        assert torch.equal(a, e) and torch.isfinite(a).all()
+
+
+def test_norm_of_more_rows_than_a_launch_is_wide():
+    """2^23 + 3 rows, a workgroup each (257 values: no whole pieces), in one call: every row is that of its first copy."""
+    rows, D = (1 << 23) + 3, 257
+    base = rand(78, "bf16")(1, D)
+    y, stats = mixer.norm_fwd(base.expand(rows, D).contiguous())
+    one, first = mixer.norm_fwd(base)
+    assert (y == one).all() and (stats == first).all()

@@ -235,3 +235,20 @@ def test_rows_of_views():
     with pytest.raises(TypeError):
         mixer._rows(_view(wide), "x", torch.bfloat16, (2, 5), (24,))
     assert qdelta.QDELTA_F32 == 0
+
+
+def test_launches_of_two_to_the_32_threads_are_refused():
+    L = mixer.lib()
+    scan = lambda fn, N, T, H, G, P, cu=None: fn(                                # noqa: E731
+        N, T, cu, H, G, P, 16, 1, 1, FAKE, H * P, FAKE, FAKE, FAKE, G * 16, FAKE, G * 16, None, None, None, FAKE, None, FAKE,
+        1 << 60, None)
+    assert scan(L.qdelta_scan_fwd, 1 << 18, 1, 8, 1, 256) == EUNSUPPORTED        # 2^23 walks of 512 threads
+    assert scan(L.qdelta_scan_fwd, 1 << 24, 1, 1, 1, 16) == EUNSUPPORTED         # 2^24 chunks, 256 threads for their gates
+    step = lambda N, H, P: L.qdelta_scan_step(                                   # noqa: E731
+        N, H, 1, P, 16, 1, 1, FAKE, H * P, FAKE, FAKE, FAKE, 16, FAKE, 16, None, None, FAKE, FAKE, FAKE, None)
+    assert step(1 << 17, 16, 128) == EUNSUPPORTED                                # 2^24 workgroups
+    assert _conv(N=1 << 24, T=0, cu=FAKE) == EUNSUPPORTED                        # 2^24 final states of 3 x 64 channels
+    nbytes = mixer.conv_workspace_bytes(1 << 23, 129, 1, 2)
+    assert L.qdelta_conv_bwd(1 << 23, 129, None, 1, 2, 1, 1, FAKE, 1, FAKE, None, None, FAKE, None, FAKE, FAKE, None, FAKE,
+                             FAKE, nbytes, None) == EUNSUPPORTED                 # 2^24 tiles of 128 tokens, one workgroup each
+    assert _conv(N=1 << 22, T=1, D=2048, ld=2048) == EUNSUPPORTED

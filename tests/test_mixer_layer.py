@@ -93,3 +93,15 @@ def test_layer_refuses_options():
 def test_layer_without_options_has_its_parameters():
     assert [n for n, _ in layer.QDeltaLayer(6, 2, 4, 3).named_parameters()] == \
         ["lambda_bias", "w_qkv.weight", "w_gates.weight", "w_out.weight"]
+
+
+def test_second_derivatives_are_refused():
+    """The backward passes are kernels without a derivative: a gradient of a gradient raises."""
+    r = rand(9)
+    x, w = r(1, 5, 3).requires_grad_(), r(3, 4).requires_grad_()
+    dt, A, B, C = r(1, 5, 1), -r(1).abs(), r(1, 5, 1, 2), r(1, 5, 1, 2)
+    for y in (layer.causal_conv(x, w)[0], layer.row_norm(x, w[:, 0].contiguous()),
+              layer.selective_scan(x[:, :, None], dt, A, B, C)[0]):
+        g, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            g.sum().backward()

@@ -27,6 +27,7 @@ namespace {
 
 // Gates of a chunk slot's 16 heads a workgroup: the raw steps are read along
 // the heads, transposed in LDS, then a token is a lane.
+// 16384 tokens of 64 heads: 12 us, 29 MB written.
 __global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
   __shared__ float raw[16][C + 1];
   const int hb = (a.H + 15) / 16, h0 = (int)(blockIdx.x % hb) * 16, t = threadIdx.x, lane = t & 63, w = wave_id(t);
@@ -88,6 +89,13 @@ struct OutLds {
 // state; waves 0 to 3 consume: outputs, then the state.  Per chunk two
 // barriers, after the operands are in LDS and at the end.  fp32 with N > 64
 // has room for one chunk in LDS only: there the two halves take turns.
+//
+// 4 x 4096 tokens, 64 heads, state 64 x 128, bf16: 225 us, one walk a CU, 3.5 us
+// a chunk (270 MB, 1.2 TB/s; 65536 tokens, 16 heads, 128 x 128: 444 us).  The
+// chain of a chunk bounds it: two barriers, vector instructions 38% of the
+// cycles (planes of the state and of the weighted x), matrix products 21%.
+// Producers and consumers on the same SIMDs fill each other's waits; all eight
+// waves doing both took 350 us.
 template <typename E, int NP>
 __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanArgs a, long items) {
   typedef OutLds<E, NP> L;
@@ -383,7 +391,10 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
 // gradient (dir 1: G = dL/dS, over dy and C from the back,
 // G <- e^{b_C} G + sum_r e^{b_r} dy_r C_r^T), over a segment or a whole
 // sequence.  Accumulators [p][n]: f4 S[nb] holds rows p = 16 w + g4 + j of
-// column n = 16 nb + col, which is also the order in `states` and `grads`.
+// column n = 16 nb + col, which is also the order in `states` and `grads`: a
+// wave's stores are whole and the backward's loads are operands as they come.
+// Both directions in one launch, 4 x 4096 tokens, 64 heads, state 64 x 128: 283
+// us for 1.08 GB written and 0.37 read (5.1 TB/s): bound by HBM.
 template <typename E, int NP>
 struct WalkLds {
   static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT);
@@ -545,7 +556,8 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_compose(ScanArgs a, int dir0) 
 
 // One token of N sequences.  A wave owns rows of one head's state, R lanes a
 // row with four consecutive n a lane and piece; the row's sum over n is formed
-// by lane moves.  Bound by the state's bytes, read and written once.
+// by lane moves.  Bound by the state's bytes, read and written once: 64 sequences
+// of 64 heads of 64 x 128 in 43 us (270 MB, 6.3 TB/s with the last level cache).
 template <typename E>
 __global__ __launch_bounds__(NTHREADS) void k_ssm_step(ScanArgs a) {
   constexpr int RPW = 4;                 // rows a wave handles at once: 16 lanes each

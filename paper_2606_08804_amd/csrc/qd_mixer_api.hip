@@ -238,7 +238,7 @@ size_t qdelta_conv_workspace_bytes(int32_t N, int32_t T, int32_t packed, int32_t
   if (N < 0 || T < 0 || D <= 0 || W < 2 || W > 4) return 0;
   static const int32_t any = 0;
   const qd::Seqs q{T, N, packed ? &any : nullptr};
-  return (size_t)qd::conv_bwd_slots(q) * (W + 1) * D * sizeof(float);
+  return (size_t)qd::conv_bwd_plan(q, D).groups * (W + 1) * D * sizeof(float);
 }
 
 int qdelta_conv_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t D, int32_t W, int32_t dtype, int32_t silu,
@@ -255,10 +255,10 @@ int qdelta_conv_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t D, 
   for (const void* p : {bias, initial_state, d_final_state, (const void*)dweight, (const void*)dbias,
                         (const void*)d_initial_state})
     if (!ok_opt(p, e)) return QDELTA_EINVAL;
-  const size_t need = (size_t)qd::conv_bwd_slots(a.q) * (W + 1) * D * sizeof(float);
+  const size_t need = (size_t)qd::conv_bwd_plan(a.q, D).groups * (W + 1) * D * sizeof(float);
   if (need > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
   if (ws_bytes < need) return QDELTA_ENOWORKSPACE;
-  if ((int64_t)qd::conv_bwd_slots(a.q) * (D + 63) * 4 + 3 * (int64_t)N * D + 256 >= kMaxThreads) return QDELTA_EUNSUPPORTED;
+  if ((int64_t)qd::conv_bwd_plan(a.q, D).groups * (D + 255) + 3 * (int64_t)N * D + 256 >= kMaxThreads) return QDELTA_EUNSUPPORTED;
   a.D = D; a.W = W; a.silu = silu != 0; a.ldx = ldx;
   a.x = x; a.w = weight; a.b = bias; a.s0 = initial_state;
   a.dy = dy; a.dsf = d_final_state;

@@ -24,11 +24,14 @@ namespace {
 // Sum over the LANES lanes of a row, the same value in each of them.
 template <int LANES>
 __device__ inline float row_sum(float x, float* red) {
-  x = sum16(x);
-  if constexpr (LANES >= 64) {
-    x += __shfl_xor(x, 16, 64);
-    x += __shfl_xor(x, 32, 64);
+  if constexpr (LANES == 8) {
+#pragma unroll
+    for (int off = 1; off < 8; off *= 2) x += __shfl_xor(x, off, 64);
+  } else {
+    x = sum16(x);
   }
+  if constexpr (LANES >= 32) x += __shfl_xor(x, 16, 64);
+  if constexpr (LANES >= 64) x += __shfl_xor(x, 32, 64);
   if constexpr (LANES == 256) {
     const int w = threadIdx.x >> 6;
     __syncthreads();                       // the last sum has been read
@@ -39,7 +42,7 @@ __device__ inline float row_sum(float x, float* red) {
   return x;
 }
 
-template <typename E, int V, int LANES, int K>
+template <typename E, int V, bool WHOLE, int LANES, int K>
 __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   __shared__ float red[4];
   constexpr int RPB = NTHREADS / LANES;
@@ -47,12 +50,12 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   const int lane = threadIdx.x % LANES;
   if (row >= a.rows) return;               // whole lane groups leave together, a workgroup that is one as a whole
   const E* x = (const E*)a.x + row * a.ldx;
-  Vec<E, V> v[K];
+  Vec<E, V, WHOLE> v[K];
   float s = 0.f;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int c = (k * LANES + lane) * V;
-    if (c < a.D) v[k].load(x + c); else v[k].zero();
+    if (c < a.D) v[k].load(x + c, a.D - c); else v[k].zero();
 #pragma unroll
     for (int i = 0; i < V; ++i) s += v[k].v[i];
   }
@@ -61,11 +64,11 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   float ss = 0.f;
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    const bool in = (k * LANES + lane) * V < a.D;
+    const int c = (k * LANES + lane) * V;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       v[k].v[i] -= mean;
-      ss += in ? v[k].v[i] * v[k].v[i] : 0.f;
+      ss += c + (WHOLE ? 0 : i) < a.D ? v[k].v[i] * v[k].v[i] : 0.f;
     }
   }
   const float r = 1.f / sqrtf(row_sum<LANES>(ss, red) * inv + a.eps);
@@ -74,10 +77,10 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   for (int k = 0; k < K; ++k) {
     const int c = (k * LANES + lane) * V;
     if (c >= a.D) break;
-    Vec<E, V> w, b, g;
-    if (a.w) w.load((const E*)a.w + c);
-    if (a.b) b.load((const E*)a.b + c);
-    if (a.g) g.load((const E*)a.g + row * a.ldg + c);
+    Vec<E, V, WHOLE> w, b, g;
+    if (a.w) w.load((const E*)a.w + c, a.D - c);
+    if (a.b) b.load((const E*)a.b + c, a.D - c);
+    if (a.g) g.load((const E*)a.g + row * a.ldg + c, a.D - c);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float o = v[k].v[i] * r;
@@ -86,7 +89,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
       if (a.g) o *= g.v[i] * fast_sigmoid(g.v[i]);
       v[k].v[i] = o;
     }
-    v[k].store(y + c);
+    v[k].store(y + c, a.D - c);
   }
   if (a.stats && lane == 0) {
     a.stats[2 * row] = mean;
@@ -94,7 +97,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
   }
 }
 
-template <typename E, int V, int LANES, int K, bool GATE>
+template <typename E, int V, bool WHOLE, int LANES, int K, bool GATE>
 __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
   __shared__ float red[4];
   extern __shared__ float cols[];          // [2][LANES * K * V] where the workgroup has more than one row
@@ -105,7 +108,8 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
   // The pieces of a row, and where registers allow it those of the next one read
   // while this one is worked on (16384 x 2048 in bf16: 49 -> 44 us).
   constexpr bool AHEAD = K * V <= (GATE ? 16 : 32) && K <= 4;
-  typedef typename Vec<E, V>::raw_t raw_t;
+  typedef Vec<E, V, WHOLE> Piece;
+  typedef typename Piece::raw_t raw_t;
   raw_t xn[K], dn[K], gn[GATE ? K : 1];
   float mean_n = 0.f, r_n = 0.f;
   auto fetch = [&](long row) {
@@ -117,9 +121,9 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
       xn[k] = dn[k] = raw_t{};
       if constexpr (GATE) gn[k] = raw_t{};
       if (c < a.D) {
-        xn[k] = *(const raw_t*)((const E*)a.x + row * a.ldx + c);
-        dn[k] = *(const raw_t*)((const E*)a.dy + row * a.D + c);
-        if constexpr (GATE) gn[k] = *(const raw_t*)((const E*)a.g + row * a.ldg + c);
+        xn[k] = Piece::fetch((const E*)a.x + row * a.ldx + c, a.D - c);
+        dn[k] = Piece::fetch((const E*)a.dy + row * a.D + c, a.D - c);
+        if constexpr (GATE) gn[k] = Piece::fetch((const E*)a.g + row * a.ldg + c, a.D - c);
       }
     }
   };
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
   if (AHEAD && row0 < a.rows) fetch(row0);
   // LANES == 256: row is uniform over the workgroup, so its barriers are met by all
   for (long row = row0; row < a.rows; row += (long)gridDim.x * RPB) {
-    Vec<E, V> xh[K], d[K], g[GATE ? K : 1];
+    Vec<E, V, WHOLE> xh[K], d[K], g[GATE ? K : 1];
     if constexpr (!AHEAD) fetch(row);
     const float mean = mean_n, r = r_n;
 #pragma unroll
@@ -145,9 +149,9 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
     for (int k = 0; k < K; ++k) {
       const int c = (k * LANES + lane) * V;
       const bool in = c < a.D;
-      Vec<E, V> w, b, o;
-      if (in && a.w) w.load((const E*)a.w + c);
-      if (GATE && in && a.b) b.load((const E*)a.b + c);
+      Vec<E, V, WHOLE> w, b, o;
+      if (in && a.w) w.load((const E*)a.w + c, a.D - c);
+      if (GATE && in && a.b) b.load((const E*)a.b + c, a.D - c);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const float h = (xh[k].v[i] - mean) * r;
@@ -173,7 +177,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
         }
       }
       if constexpr (GATE)
-        if (in) o.store((E*)a.dg + row * a.D + c);
+        if (in) o.store((E*)a.dg + row * a.D + c, a.D - c);
     }
     s1 = a.rms ? 0.f : row_sum<LANES>(s1, red) * inv;
     s2 = row_sum<LANES>(s2, red) * inv;
@@ -183,20 +187,18 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
       if (c >= a.D) break;
 #pragma unroll
       for (int i = 0; i < V; ++i) d[k].v[i] = r * (d[k].v[i] - s1 - xh[k].v[i] * s2);
-      d[k].store((E*)a.dx + row * a.D + c);
+      d[k].store((E*)a.dx + row * a.D + c, a.D - c);
     }
   }
   if (!a.part) return;
   // one partial row [2][D] per workgroup: over the rows of a wave by lane moves, over the waves in order
-  if constexpr (LANES == 16) {
+#pragma unroll
+  for (int off = LANES; off < 64; off *= 2)
 #pragma unroll
     for (int i = 0; i < K * V; ++i) {
-      dw[i] += __shfl_xor(dw[i], 16, 64);
-      dw[i] += __shfl_xor(dw[i], 32, 64);
-      db[i] += __shfl_xor(db[i], 16, 64);
-      db[i] += __shfl_xor(db[i], 32, 64);
+      dw[i] += __shfl_xor(dw[i], off, 64);
+      db[i] += __shfl_xor(db[i], off, 64);
     }
-  }
   float* out = a.part + (long)blockIdx.x * 2 * a.D;
   if constexpr (LANES < 256) {
     constexpr int N = LANES * K * V;
@@ -256,42 +258,47 @@ __global__ __launch_bounds__(CS_COLS* CS_ROWS) void k_colsum(const float* __rest
   else b[d] = fromf<E>(s);
 }
 
-template <typename E, int V, int LANES, int K>
+template <typename E, int V, bool WHOLE, int LANES, int K>
 hipError_t fwd(const RowNormArgs& a, hipStream_t st) {
   constexpr int RPB = NTHREADS / LANES;
   const long blocks = (a.rows + RPB - 1) / RPB, wide = 1L << 23;     // a launch's dimension has less than 2^32 threads
   const dim3 grid((unsigned)(blocks < wide ? blocks : wide), (unsigned)((blocks + wide - 1) / wide));
-  hipLaunchKernelGGL((k_norm_fwd<E, V, LANES, K>), grid, dim3(NTHREADS), 0, st, a);
+  hipLaunchKernelGGL((k_norm_fwd<E, V, WHOLE, LANES, K>), grid, dim3(NTHREADS), 0, st, a);
   return hipGetLastError();
 }
 
-template <typename E, int V, int LANES, int K>
+template <typename E, int V, bool WHOLE, int LANES, int K>
 hipError_t bwd(const RowNormArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)norm_bwd_blocks(a.rows, a.D));
   const size_t lds = LANES < 256 ? 2 * sizeof(float) * LANES * K * V : 0;
-  if (a.g) hipLaunchKernelGGL((k_norm_bwd<E, V, LANES, K, true>), grid, dim3(NTHREADS), lds, st, a);
-  else hipLaunchKernelGGL((k_norm_bwd<E, V, LANES, K, false>), grid, dim3(NTHREADS), lds, st, a);
+  if (a.g) hipLaunchKernelGGL((k_norm_bwd<E, V, WHOLE, LANES, K, true>), grid, dim3(NTHREADS), lds, st, a);
+  else hipLaunchKernelGGL((k_norm_bwd<E, V, WHOLE, LANES, K, false>), grid, dim3(NTHREADS), lds, st, a);
   return hipGetLastError();
 }
 
-// Lanes a row by its pieces: 16 lanes of one, a wave of one or four, else the
-// workgroup (rows of 256 pieces by the workgroup, one each: backward 56 us
-// instead of 49, its sums meet barriers).
+// Lanes a row by its pieces: the fewest of 8 to 64 that hold one each, a wave
+// with two or four, else the workgroup (rows of 256 pieces by the workgroup, one
+// each: backward 56 us instead of 49, its sums meet barriers).  A variant twice as
+// wide as the row runs half of its lanes or registers for nothing (forward and
+// backward in bf16, next wider and its own: 524288 gated rows of 64 152 and 104
+// us, 131072 of 200 150 and 92, 16384 rows of 1024 59 and 49, of 4096 227 and 196).
 #define QD_ROWNORM(FN)                                             \
   const int nv = (a.D + V - 1) / V;                                \
-  if (nv <= 16) return FN<E, V, 16, 1>(a, st);                     \
-  if (nv <= 64) return FN<E, V, 64, 1>(a, st);                     \
-  if (nv <= 256) return FN<E, V, 64, 4>(a, st);                    \
-  if (nv <= 1024) return FN<E, V, 256, 4>(a, st);                  \
+  if (nv <= 8) return FN<E, V, WHOLE, 8, 1>(a, st);                \
+  if (nv <= 16) return FN<E, V, WHOLE, 16, 1>(a, st);              \
+  if (nv <= 32) return FN<E, V, WHOLE, 32, 1>(a, st);              \
+  if (nv <= 64) return FN<E, V, WHOLE, 64, 1>(a, st);              \
+  if (nv <= 128) return FN<E, V, WHOLE, 64, 2>(a, st);             \
+  if (nv <= 256) return FN<E, V, WHOLE, 64, 4>(a, st);             \
+  if (nv <= 512) return FN<E, V, WHOLE, 256, 2>(a, st);            \
+  if (nv <= 1024) return FN<E, V, WHOLE, 256, 4>(a, st);           \
   if constexpr (V == 4)                                            \
-    if (nv <= 2048) return FN<E, V, 256, 8>(a, st);                \
-  if constexpr (V == 1)                                            \
-    if (nv <= 8192) return FN<E, V, 256, 32>(a, st);               \
+    if (nv <= 2048) return FN<E, V, WHOLE, 256, 8>(a, st);         \
   return hipErrorInvalidValue
 
-template <typename E, int V>
+template <typename E, int V, bool WHOLE>
 hipError_t by_size_fwd(const RowNormArgs& a, hipStream_t st) { QD_ROWNORM(fwd); }
-template <typename E, int V>
+template <typename E, int V, bool WHOLE>
 hipError_t by_size_bwd(const RowNormArgs& a, hipStream_t st) { QD_ROWNORM(bwd); }
 #undef QD_ROWNORM
 
@@ -317,14 +324,14 @@ int norm_bwd_blocks(long rows, int D) {
 }
 
 hipError_t launch_norm_fwd(const RowNormArgs& a, int dtype, hipStream_t st) {
-  if (dtype == 1) return whole(a, 2) ? by_size_fwd<__bf16, 8>(a, st) : by_size_fwd<__bf16, 1>(a, st);
-  return whole(a, 4) ? by_size_fwd<float, 4>(a, st) : by_size_fwd<float, 1>(a, st);
+  if (dtype == 1) return whole(a, 2) ? by_size_fwd<__bf16, 8, true>(a, st) : by_size_fwd<__bf16, 8, false>(a, st);
+  return whole(a, 4) ? by_size_fwd<float, 4, true>(a, st) : by_size_fwd<float, 4, false>(a, st);
 }
 
 hipError_t launch_norm_bwd(const RowNormArgs& a, int dtype, hipStream_t st) {
   hipError_t e;
-  if (dtype == 1) e = whole(a, 2) ? by_size_bwd<__bf16, 8>(a, st) : by_size_bwd<__bf16, 1>(a, st);
-  else e = whole(a, 4) ? by_size_bwd<float, 4>(a, st) : by_size_bwd<float, 1>(a, st);
+  if (dtype == 1) e = whole(a, 2) ? by_size_bwd<__bf16, 8, true>(a, st) : by_size_bwd<__bf16, 8, false>(a, st);
+  else e = whole(a, 4) ? by_size_bwd<float, 4, true>(a, st) : by_size_bwd<float, 4, false>(a, st);
   if (e != hipSuccess || !a.part) return e;
   return launch_colsum(a.part, norm_bwd_blocks(a.rows, a.D), 2, 1, a.D, dtype, a.dw, a.db, st);
 }

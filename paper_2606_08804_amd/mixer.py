@@ -36,7 +36,7 @@ EXPORTS = (
 )
 
 _lib = None
-_p, _need, _opt, _dt, _workspace = _q._p, _q._need, _q._opt, _q._dt, _q._workspace
+_p, _need, _opt, _dt = _q._p, _q._need, _q._opt, _q._dt
 
 
 def lib():
@@ -85,6 +85,10 @@ def _one_device(first, *others):
         if t is not None and t.get_device() != index:
             raise ValueError(f"tensors on {first.device} and {t.device}: all of a call's live on one device")
     return first.device
+
+
+def _workspace(nbytes, device, workspace):
+    return _q._workspace(nbytes, device, _opt(workspace, "workspace"))
 
 
 def _rows(t, name, dtype, lead, size):

@@ -335,9 +335,45 @@ def test_tokens_behind_the_last_sequence(monkeypatch, dtype):
 
 
 def test_norm_of_more_rows_than_a_launch_is_wide():
-    """2^23 + 3 rows, a workgroup each (257 values: no whole pieces), in one call: every row is that of its first copy."""
-    rows, D = (1 << 23) + 3, 257
+    """2^27 + 3 rows of 3 values, 16 to a workgroup: 2^23 + 1 workgroups of 256 threads, past the 2^32 of one dimension of a
+    launch.  Every row is that of its first copy."""
+    rows, D = (1 << 27) + 3, 3
     base = rand(78, "bf16")(1, D)
     y, stats = mixer.norm_fwd(base.expand(rows, D).contiguous())
     one, first = mixer.norm_fwd(base)
     assert (y == one).all() and (stats == first).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_workspaces_are_whole(dtype):
+    """A workspace that is a view with gaps or one element expanded is refused before any launch."""
+    r = rand(79, dtype)
+    x, w, dy = r(2, 40, 24), r(24, 4), r(2, 40, 24)
+    nbytes = mixer.conv_workspace_bytes(2, 40, 24, 4)
+    for ws in (torch.zeros(1, dtype=torch.uint8, device="cuda").expand(nbytes),
+               torch.zeros(2 * nbytes, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            mixer.conv_bwd(x, w, None, None, dy, workspace=ws)
+    with pytest.raises(ValueError):
+        mixer.conv_bwd(x, w, None, None, dy, workspace=torch.zeros(nbytes, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [1, 3, 5, 9, 15, 17, 31, 63, 65, 127, 129, 1023, 2047, 2049, 8191])
+def test_norm_rows_of_any_width(D, dtype):
+    """Widths about the pieces' and the lanes' edges, the rows between other values that must stay out of the results."""
+    r = rand(80 + D, dtype)
+    rows = 5
+    x, g = r(rows, D + 3)[:, 1:D + 1], r(rows, D + 1)[:, :D]
+    w, b, dy = r(D), r(D), r(rows, D)
+    y, stats = mixer.norm_fwd(x, w, b, g)
+    d = mixer.norm_bwd(x, w, b, g, stats, dy)
+    y2, stats2 = mixer.norm_fwd(x.contiguous(), w, b, g.contiguous())
+    assert torch.equal(y, y2) and torch.equal(stats, stats2)
+    assert all(torch.equal(d[k], v) for k, v in mixer.norm_bwd(x.contiguous(), w, b, g.contiguous(), stats, dy).items())
+    n = lambda t: t.double().cpu().numpy()                                       # noqa: E731
+    xs, mag = n(x), np.abs(n(x)) + np.abs(n(x)).mean(1, keepdims=True)
+    rs = 1 / np.sqrt(((xs - xs.mean(1, keepdims=True)) ** 2).mean(1, keepdims=True) + 1e-5)
+    gate = n(g) / (1 + np.exp(-n(g)))
+    want = ((xs - xs.mean(1, keepdims=True)) * rs * n(w) + n(b)) * gate
+    close(y, want, (mag * rs * np.abs(n(w)) + np.abs(n(b))) * np.abs(gate), "y")

@@ -29,7 +29,7 @@
 // A spilled register costs more than its own bytes: its reload waits for every
 // prefetch issued before it.
 //
-// 4 x 4096 tokens, 64 heads of one group, state 64 x 128, bf16: 495 us, 7.7 us a
+// 4 x 4096 tokens, 64 heads of one group, state 64 x 128, bf16: 500 us, 7.8 us a
 // chunk and head.  States and gradients are 1.08 of the 1.57 GB it moves (3.2
 // TB/s); vector instructions take 46% of the cycles and matrix products 19%,
 // on two waves a SIMD, which the registers (256 each) and LDS allow.

@@ -6,9 +6,11 @@
 // is an operand as it stands (its rows become k), without a trip through LDS.
 // bf16 takes one 16x16x32 instruction a step, fp32 eight 16x16x4 ones.
 //
-// A fp32 value enters a bf16 product as a sum of bf16 values ("planes"):
-// x = hi + lo is off by 2^-16 at most, x = hi + mid + lo is exact.  Two planes
-// where the result is rounded to bf16, three where it is fp32.
+// A fp32 value enters a bf16 product as a sum of three bf16 values ("planes"),
+// x = hi + mid + lo, which is exact.  Two of them are off by up to 2^-16: results
+// that are rounded to bf16 afterwards then differ from those of fp32 products in
+// one of 500 (dB, dC) to 1500 values (y), and cost a tenth less (4 x 4096 tokens, 64
+// heads, training 1012 us instead of 1103; a prompt of 65536, 16 heads, 594 and 675).
 #pragma once
 
 #include "qd_mixer.h"

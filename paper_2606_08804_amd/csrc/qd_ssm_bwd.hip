@@ -41,7 +41,7 @@ namespace {
 
 template <typename E, int NP>
 struct BwdLds {
-  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDX = steps_ld<E>(PT), PL = sizeof(E) == 2 ? 2 : 1;
+  static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDX = steps_ld<E>(PT), PL = Planes<E, 3>::N;
   static constexpr int LDS_ = lds_ld<float>(NP), LDT = sizeof(E) == 4 && NP == 128 ? PT : lds_ld<float>(PT);   // (no room for padding there)
   E B[C * LDN], Cm[C * LDN], dY[C * LDP];
   E X[C * LDX];                      // steps
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
             }
           }
         }
-        const Planes<E, 2> ep = planes<E, 2>(e[0], e[1]);
+        const Planes<E, 3> ep = planes<E, 3>(e[0], e[1]);
 #pragma unroll
         for (int b4 = 0; b4 < NB; b4 += 4) {
           Fr<E> bt[4];
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
           for (int b = 0; b < 4; ++b) bt[b] = col_frag<E>(s.B, L::LDN, 32 * pair, 16 * (b4 + b), lane);
           phase();
 #pragma unroll
-          for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+          for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
 #pragma unroll
             for (int b = 0; b < 4; ++b) acc[b4 + b] = mma(bt[b], ep.p[pl], acc[b4 + b]);
         }
@@ -510,17 +510,17 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
         }
       }
       {
-        const Planes<E, 2> wp = planes<E, 2>(wk[0], wk[1]);
+        const Planes<E, 3> wp = planes<E, 3>(wk[0], wk[1]);
         Fr<E> yt[4];
 #pragma unroll
         for (int b = 0; b < 4; ++b) yt[b] = col_frag<E>(s.dY, L::LDP, 32 * pair, 16 * b, lane);
         phase();
 #pragma unroll
-        for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+        for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
 #pragma unroll
           for (int b = 0; b < 4; ++b) xacc[b] = mma(yt[b], wp.p[pl], xacc[b]);
       }
-      const Planes<E, 2> ep = planes<E, 2>(e[0], e[1]);
+      const Planes<E, 3> ep = planes<E, 3>(e[0], e[1]);
 #pragma unroll
       for (int b4 = 0; b4 < NB; b4 += 4) {
         Fr<E> ct[4];
@@ -528,7 +528,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
         for (int b = 0; b < 4; ++b) ct[b] = col_frag<E>(s.Cm, L::LDN, 32 * pair, 16 * (b4 + b), lane);
         phase();
 #pragma unroll
-        for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+        for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
 #pragma unroll
           for (int b = 0; b < 4; ++b) acc[b4 + b] = mma(ct[b], ep.p[pl], acc[b4 + b]);
       }

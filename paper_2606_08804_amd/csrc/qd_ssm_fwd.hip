@@ -72,7 +72,7 @@ __device__ inline bool not_finite(u32x4 v) {
 template <typename E, int NP>
 struct OutLds {
   static constexpr int LDN = lds_ld<E>(NP), LDP = lds_ld<E>(PT), LDM = steps_ld<E>(NP), LDC = steps_ld<E>(C),
-                       PL = sizeof(E) == 2 ? 2 : 1;
+                       PL = Planes<E, 3>::N;
   struct Buf {
     E B[C * LDN], X[C * LDP];
     E Cm[C * LDM];                     // steps
@@ -293,9 +293,9 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
         for (int b = 0; b < 4; ++b) cf[0][b] = step_frag<E>(u.Cm, L::LDM, 16 * b, 32 * k, lane);
         phase();
       }
-      const Planes<E, 2> sp = planes<E, 2>(S[2 * k], S[2 * k + 1]);
+      const Planes<E, 3> sp = planes<E, 3>(S[2 * k], S[2 * k + 1]);
 #pragma unroll
-      for (int pl = Planes<E, 2>::N - 1; pl >= 0; --pl)
+      for (int pl = Planes<E, 3>::N - 1; pl >= 0; --pl)
 #pragma unroll
         for (int b = 0; b < 4; ++b) o[b] = mma(sp.p[pl], cf[AHEAD ? k : 0][b], o[b]);
     }

@@ -18,7 +18,11 @@
  *
  * Sizes: a call has less than 2^31 tokens (N T where dense), and one whose
  * launches would need 2^32 threads or more is QDELTA_EUNSUPPORTED (for the scan
- * about 2^23 heads over all sequences, or 2^31 over all tokens). */
+ * about 2^23 heads over all sequences, or 2^31 over all tokens).
+ *
+ * Precision: sums, statistics and states are fp32.  Exponentials (SiLU, softplus,
+ * decays) are good to the last place of fp32; with bf16 activations those of SiLU
+ * and of the decays between tokens of a chunk are off by |x| 2^-23. */
 #ifndef QDELTA_MIXER_H
 #define QDELTA_MIXER_H
 

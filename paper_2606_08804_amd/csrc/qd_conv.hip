@@ -94,7 +94,7 @@ __global__ __launch_bounds__(NTHREADS) void k_conv_fwd(ConvArgs a, int L, long t
         float u = b[e];
 #pragma unroll
         for (int j = 0; j < W; ++j) u += w[j][e] * x[k + j].v[e];
-        o.v[e] = a.silu ? u * fast_sigmoid(u) : u;
+        o.v[e] = a.silu ? u * sigmoid<E>(u) : u;
       }
       o.store(y + (long)(pos + k) * a.D, a.D - c);
     }
@@ -104,9 +104,10 @@ __global__ __launch_bounds__(NTHREADS) void k_conv_fwd(ConvArgs a, int L, long t
 }
 
 // du from u and dy.
+template <typename E>
 __device__ inline float act_grad(float u, float dy, int silu) {
   if (!silu) return dy;
-  const float sg = fast_sigmoid(u);
+  const float sg = sigmoid<E>(u);
   return dy * (sg * (1.f + u * (1.f - sg)));
 }
 
@@ -144,7 +145,7 @@ __device__ inline void initial_grad(const ConvArgs& a, long k) {
         u += w[j][e] * x[t + j].v[e];
         if (j == i - t) tap = w[j][e];
       }
-      o.v[e] += tap * act_grad(u, g.v[e], a.silu);
+      o.v[e] += tap * act_grad<E>(u, g.v[e], a.silu);
     }
   }
   o.store((E*)a.ds0 + ((long)n * (W - 1) + i) * a.D + c, a.D - c);
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(NTHREADS) void k_conv_bwd(ConvArgs a, int cgroups, 
           float u = b[e];
 #pragma unroll
           for (int j = 0; j < W; ++j) u += w[j][e] * x[k + j].v[e];
-          const float d = t < stop ? act_grad(u, g.v[e], a.silu) : 0.f;
+          const float d = t < stop ? act_grad<E>(u, g.v[e], a.silu) : 0.f;
           du[W - 1 + k][e] = d;
           if (t < end) {
 #pragma unroll
@@ -272,7 +273,7 @@ __global__ __launch_bounds__(64) void k_conv_step(ConvArgs a) {
     float u = b[e];
 #pragma unroll
     for (int j = 0; j < W; ++j) u += w[j][e] * x[j].v[e];
-    o.v[e] = a.silu ? u * fast_sigmoid(u) : u;
+    o.v[e] = a.silu ? u * sigmoid<E>(u) : u;
   }
   o.store((E*)a.y + (long)n * a.D + c, a.D - c);
 #pragma unroll

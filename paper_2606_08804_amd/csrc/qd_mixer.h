@@ -58,11 +58,20 @@ struct Vec {
   }
 };
 
-// sigmoid and x sigmoid(x) from the hardware's exponential and reciprocal
-// (one unit in the last place each): relative error below 2^-20 for |x| < 16,
-// and 0 or 1 where the exponential leaves the range of fp32.
+// exp, and the sigmoid from it and the hardware's reciprocal (one unit in the last
+// place; 0 or 1 where the exponential leaves the range of fp32).  With bf16
+// activations exp is the hardware's 2^t of the rounded t = x log2(e), off by
+// |x| 2^-23 relative: below 2^-18 for every decay or sigmoid above e^-32, in sums
+// whose bf16 operands are themselves rounded by 2^-8.  With fp32 activations, and for
+// decays of the fp32 state in either type, it is the library's, good to the last
+// place at every x (65536 gated rows of 1024 in fp32, forward: 141.3 -> 142.5 us;
+// the scan of 4 x 4096 tokens, 16 heads, 64 x 64 in fp32: 143 -> 150).
 __device__ inline float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-__device__ inline float fast_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + fast_exp(-x)); }
+template <typename E> __device__ inline float exp_of(float x) {
+  if constexpr (sizeof(E) == 2) return fast_exp(x);
+  else return expf(x);
+}
+template <typename E> __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_of<E>(-x)); }
 
 // Sequences of a call: dense (cu == nullptr: N sequences of T tokens) or
 // packed (T tokens in all, cu[N + 1] on the device).  Tiles of L consecutive

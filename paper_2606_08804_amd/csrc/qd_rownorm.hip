@@ -86,7 +86,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_fwd(RowNormArgs a) {
       float o = v[k].v[i] * r;
       if (a.w) o *= w.v[i];
       if (a.b) o += b.v[i];
-      if (a.g) o *= g.v[i] * fast_sigmoid(g.v[i]);
+      if (a.g) o *= g.v[i] * sigmoid<E>(g.v[i]);
       v[k].v[i] = o;
     }
     v[k].store(y + c, a.D - c);
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(NTHREADS) void k_norm_bwd(RowNormArgs a) {
         const float h = (xh[k].v[i] - mean) * r;
         float e = d[k].v[i];
         if constexpr (GATE) {
-          const float gv = g[k].v[i], sg = fast_sigmoid(gv);
+          const float gv = g[k].v[i], sg = sigmoid<E>(gv);
           float lin = h;
           if (a.w) lin *= w.v[i];
           if (a.b) lin += b.v[i];

@@ -388,13 +388,13 @@ __device__ inline float step_size(float z, int softplus) {
   return softplus ? fmaxf(z, 0.f) + log1pf(expf(-fabsf(z))) : z;
 }
 // exp(b_r - b_i).
-__device__ inline float decay(float hr, float lr, float hi, float li) { return fast_exp((hr - hi) + (lr - li)); }
+template <typename E> __device__ inline float decay(float hr, float lr, float hi, float li) { return exp_of<E>((hr - hi) + (lr - li)); }
 
 // exp of b's step from the end of block i to the end of the block before r's
 // (i < r, blocks of 16): what head16 and tail16 leave out of exp(b_r - b_i).
-__device__ inline float between(const Gates& g, int r, int i) {
+template <typename E> __device__ inline float between(const Gates& g, int r, int i) {
   const int e = 16 * r - 1, f = 16 * i + 15;
-  return decay(g.bh[e], g.bl[e], g.bh[f], g.bl[f]);
+  return decay<E>(g.bh[e], g.bl[e], g.bh[f], g.bl[f]);
 }
 
 hipError_t launch_scan_gates(const ScanArgs& a, hipStream_t st);

@@ -332,12 +332,12 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
           for (int k = 0; k < 2; ++k) xf[k] = step_frag<E>(s.X, L::LDX, 16 * b, 32 * k, lane);
           f4 wt;
           if (b < w) {
-            wt = (h16 * between(s.g, w, b)) * *(const f4*)(s.g.tail16 + 16 * b + g4);
+            wt = (h16 * between<E>(s.g, w, b)) * *(const f4*)(s.g.tail16 + 16 * b + g4);
           } else {
             const f4 hi = *(const f4*)(s.g.bh + 16 * b + g4), li = *(const f4*)(s.g.bl + 16 * b + g4);
             const float hr = s.g.bh[own], lr = s.g.bl[own];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wt[j] = g4 + j <= col ? decay(hr, lr, hi[j], li[j]) : 0.f;
+            for (int j = 0; j < 4; ++j) wt[j] = g4 + j <= col ? decay<E>(hr, lr, hi[j], li[j]) : 0.f;
           }
           wt *= *(const f4*)(s.g.dt + 16 * b + g4);
 #pragma unroll
@@ -484,12 +484,12 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanAr
         for (int k = 0; k < 2; ++k) yf[k] = row_frag<E>(s.dY, L::LDP, 16 * b, 32 * k, lane);
         f4 wt;
         if (b > w) {
-          wt = (t16 * between(s.g, b, w)) * *(const f4*)(s.g.head16 + 16 * b + g4);
+          wt = (t16 * between<E>(s.g, b, w)) * *(const f4*)(s.g.head16 + 16 * b + g4);
         } else {
           const f4 hr = *(const f4*)(s.g.bh + 16 * b + g4), lr = *(const f4*)(s.g.bl + 16 * b + g4);
           const float hi = s.g.bh[own], li = s.g.bl[own];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) wt[j] = g4 + j >= col ? decay(hr[j], lr[j], hi, li) : 0.f;
+          for (int j = 0; j < 4; ++j) wt[j] = g4 + j >= col ? decay<E>(hr[j], lr[j], hi, li) : 0.f;
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) e[b2] = mma(yf[k], xf[k], e[b2]);

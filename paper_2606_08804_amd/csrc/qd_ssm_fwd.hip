@@ -51,10 +51,10 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
     g[2 * C] = (float)(b - (double)(float)b);
     // each from a difference formed in 64 bits
     const double before = __shfl(b, max(lane & ~15, 1) - 1, 64);
-    g[3 * C] = fast_exp((float)b);
-    g[4 * C] = fast_exp((float)(__shfl(b, C - 1, 64) - b));
-    g[5 * C] = fast_exp((float)(lane < 16 ? b : b - before));
-    g[6 * C] = fast_exp((float)(__shfl(b, lane | 15, 64) - b));
+    g[3 * C] = expf((float)b);
+    g[4 * C] = expf((float)(__shfl(b, C - 1, 64) - b));
+    g[5 * C] = expf((float)(lane < 16 ? b : b - before));
+    g[6 * C] = expf((float)(__shfl(b, lane | 15, 64) - b));
   }
 }
 
@@ -185,7 +185,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
           const int i0 = 32 * pair + 16 * b;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            v[b][j] = i0 + g4 + j <= r ? v[b][j] * (decay(hr, lr, hi[b][j], li[b][j]) * dt[b][j]) : 0.f;
+            v[b][j] = i0 + g4 + j <= r ? v[b][j] * (decay<E>(hr, lr, hi[b][j], li[b][j]) * dt[b][j]) : 0.f;
           put_planes<E, PL>(u.W[0] + r * L::LDC + step_at<E>(i0 + g4), C * L::LDC, v[b]);
         }
       }
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_compose(ScanArgs a, int dir0) 
   for (int j = 0; j < k; ++j) {
     const long slot = base + (dir ? k - 1 - j : j), u = slot * a.H + h;
     a.entry[dir][u * per + i] = S;
-    S = fast_exp(a.decay[u]) * S + a.total[dir][u * per + i];
+    S = expf(a.decay[u]) * S + a.total[dir][u * per + i];
   }
   float* out = dir ? a.dS0 : a.Sf;
   if (out) out[at] = S;
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_step(ScanArgs a) {
   const int p = (int)(blockIdx.x % per) * 4 * RPW + w * RPW + (lane >> 4), l = lane & 15;
   const int grp = h / (a.H / a.G);
   const float z = a.dt[unit] + (a.bias ? a.bias[h] : 0.f);
-  const float dt = step_size(z, a.softplus), al = fast_exp(dt * a.A[h]);
+  const float dt = step_size(z, a.softplus), al = expf(dt * a.A[h]);
   if (p >= a.P) return;
   const float x = tof(((const E*)a.x)[n * a.ldx + (long)h * a.P + p]), dx = dt * x;
   const E* B = (const E*)a.B + n * a.ldb + (long)grp * a.N;

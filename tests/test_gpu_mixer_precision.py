@@ -44,3 +44,59 @@ def test_scan_in_bf16_takes_fp32_values_whole(P, N):
                dB=bwd((1.0, 1.0, 1.0), None, one, PARTS)["dB"].view(-1)[n].item(),
                dC=bwd((1.0, 1.0, 1.0), one, None, PARTS)["dC"].view(-1)[n].item())
     assert got == {k: UP for k in got}
+
+
+# An exponential good to one place (2^-23), 1 + it, a reciprocal good to one place and one or two products: below 2^-21.
+K_EXP = 2.0 ** -21
+POINTS = torch.cat([torch.linspace(-85, 0, 511), torch.linspace(0.01, 40, 129)])
+
+
+def _off(got, want, scale=None):
+    return float(((got.double().cpu() - want).abs() / (want.abs() if scale is None else scale).clamp(min=1e-37)).max())
+
+
+@pytest.mark.parametrize("D", [POINTS.numel(), POINTS.numel() - 1])           # rows of whole pieces, and others
+def test_silu_in_fp32_is_good_to_the_last_places(D):
+    """SiLU and its derivative relative to their own size, far below zero too: the convolution with the taps 0 and 1,
+    the norm of rows (1, -1) (mean 0, deviation 1) under the gate."""
+    u = POINTS[:D].double()
+    sg = 1 / (1 + torch.exp(-u))
+    want, slope, terms = u * sg, sg * (1 + u * (1 - sg)), sg * (1 + u.abs())
+    x = POINTS[:D].cuda()[None, None]
+    w = torch.tensor([0.0, 1.0], device="cuda").repeat(D, 1)
+    y, state = mixer.conv_fwd(x, w, activation="silu")
+    assert _off(y[0, 0], want) <= K_EXP
+    assert _off(mixer.conv_step(x[0], w, None, torch.zeros_like(state), activation="silu")[0], want) <= K_EXP
+    dx = mixer.conv_bwd(x, w, None, None, torch.ones_like(x), activation="silu")["dx"]
+    assert _off(dx[0, 0], slope, terms) <= 2 * K_EXP                  # two more roundings, and 1 - sg is off by one of 1
+    rows = torch.tensor([1.0, -1.0], device="cuda").repeat(D, 1)
+    gate = x[0, 0, :, None].expand(D, 2).contiguous()
+    y, stats = mixer.norm_fwd(rows, gate=gate, eps=0.0)
+    assert (stats == torch.tensor([0.0, 1.0], device="cuda")).all()
+    assert _off(y[:, 0], want) <= K_EXP and _off(-y[:, 1], want) <= K_EXP
+    dg = mixer.norm_bwd(rows, None, None, gate, stats, torch.ones_like(rows))["dgate"]
+    assert _off(dg[:, 0], slope, terms) <= 2 * K_EXP
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_scan_decays_of_the_state_are_good_to_the_last_places(dtype):
+    """A state of ones after one token that adds nothing is exp(dt A), for prompts, their state's gradient and single
+    tokens; in fp32 the output of the token after one that came in is that as well."""
+    H, P, N = 64, 4, 4
+    A = -torch.linspace(0.125, 80, H).cuda()
+    want = torch.exp(A.double().cpu())
+    z = lambda *s, t=dtype: torch.zeros(s, dtype=t, device="cuda")                # noqa: E731
+    ones = torch.ones(1, H, P, N, device="cuda")
+    dt = torch.ones(1, 1, H, device="cuda")
+    args = (z(1, 1, H, P), dt, A, z(1, 1, 1, N), z(1, 1, 1, N))
+    _, s = mixer.scan_fwd(*args, initial_state=ones)
+    g = mixer.scan_bwd(*args, None, None, ones, z(1, 1, H, P), ones)
+    one = ones.clone()
+    mixer.scan_step(*(t[0] if t.dim() > 1 else t for t in args), one)
+    for got in (s, g["d_initial_state"], one):
+        assert (got == got[:, :, :1, :1]).all() and _off(got[0, :, 0, 0], want) <= K_EXP
+    if dtype == torch.float32:
+        x, B, C = z(1, 2, H, P), z(1, 2, 1, N), z(1, 2, 1, N)
+        x[:, 0], B[:, 0], C[:, 1, 0, 0] = 1, 1, 1
+        y, _ = mixer.scan_fwd(x, dt.expand(1, 2, H).contiguous(), A, B, C)
+        assert not y[:, 0].any() and _off(y[0, 1, :, 0], want) <= 2 * K_EXP       # products in three more roundings

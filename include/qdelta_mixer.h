@@ -16,9 +16,10 @@
  * the outputs stay as they are.  A malformed cu_seqlens leaves the outputs of
  * the sequences concerned unspecified; memory is never accessed out of bounds.
  *
- * Sizes: a call has less than 2^31 tokens (N T where dense), and one whose
- * launches would need 2^32 threads or more is QDELTA_EUNSUPPORTED (for the scan
- * about 2^23 heads over all sequences, or 2^31 over all tokens).
+ * Sizes: a call has less than 2^31 tokens (N T where dense) with T at most
+ * 2^31 - 64, and one whose launches would need 2^32 threads or more is
+ * QDELTA_EUNSUPPORTED (for the scan about 2^23 heads over all sequences, 2^23
+ * groups over all chunks of 64 tokens, or 2^31 heads over all tokens).
  *
  * Precision: sums, statistics and states are fp32.  Exponentials (SiLU, softplus,
  * decays) are good to the last place of fp32; with bf16 activations those of SiLU

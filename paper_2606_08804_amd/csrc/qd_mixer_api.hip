@@ -15,6 +15,11 @@ bool ok_opt(const void* p, int size) { return p == nullptr || ok_ptr(p, size); }
 int elem_size(int32_t dtype) { return dtype == QDELTA_BF16 ? 2 : 4; }
 int status(hipError_t e) { return e == hipSuccess ? QDELTA_OK : QDELTA_EHIP; }
 
+// Tokens of a sequence (of the whole call where packed).  Positions are counted in
+// 32 bits, and a tile of the convolution (64 tokens at most) that starts before
+// token T ends before T + 64.  (The scan's launches end at 2^29 tokens.)
+constexpr int64_t kMaxLength = (int64_t(1) << 31) - 64;
+
 int check_seqs(int32_t N, int32_t T, const int32_t* cu, qd::Seqs& q) {
   if (N < 0 || T < 0 || !ok_opt(cu, 4)) return QDELTA_EINVAL;
   if (cu && N == 0 && T > 0) return QDELTA_EINVAL;
@@ -22,6 +27,7 @@ int check_seqs(int32_t N, int32_t T, const int32_t* cu, qd::Seqs& q) {
   q.T = T;
   q.cu = cu;
   // row numbers stay within 32 bits
+  if (T > kMaxLength) return QDELTA_EUNSUPPORTED;
   if ((cu ? (int64_t)T : (int64_t)N * T) >= (int64_t(1) << 31)) return QDELTA_EUNSUPPORTED;
   return QDELTA_OK;
 }
@@ -235,9 +241,9 @@ int qdelta_conv_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t D, 
 }
 
 size_t qdelta_conv_workspace_bytes(int32_t N, int32_t T, int32_t packed, int32_t D, int32_t W) {
-  if (N < 0 || T < 0 || D <= 0 || W < 2 || W > 4) return 0;
   static const int32_t any = 0;
-  const qd::Seqs q{T, N, packed ? &any : nullptr};
+  qd::Seqs q;
+  if (check_seqs(N, T, packed ? &any : nullptr, q) || check_conv(q, D, W, QDELTA_F32, INT64_MAX)) return 0;
   return (size_t)qd::conv_bwd_plan(q, D).groups * (W + 1) * D * sizeof(float);
 }
 

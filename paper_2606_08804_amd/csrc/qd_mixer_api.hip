@@ -41,6 +41,7 @@ int check_conv(const qd::Seqs& q, int32_t D, int32_t W, int32_t dtype, int64_t l
   if (D <= 0 || W <= 0 || ldx < D) return QDELTA_EINVAL;
   if (dtype != QDELTA_F32 && dtype != QDELTA_BF16) return QDELTA_EINVAL;
   if (W < 2 || W > 4) return QDELTA_EUNSUPPORTED;
+  if ((int64_t)D * W >= (int64_t(1) << 31)) return QDELTA_EUNSUPPORTED;   // the taps are counted in 32 bits
   // threads of the forward and the step in single channels; tiles shorter than
   // 64 tokens are taken up to 2^17 threads of tiles of 64
   if ((q.slots(64) + 3 * (int64_t)q.N) * D + (int64_t(1) << 20) >= kMaxThreads) return QDELTA_EUNSUPPORTED;
@@ -265,6 +266,8 @@ int qdelta_conv_bwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t D, 
   if (need > 0 && !ok_ptr(ws, 16)) return QDELTA_EINVAL;
   if (ws_bytes < need) return QDELTA_ENOWORKSPACE;
   if ((int64_t)qd::conv_bwd_plan(a.q, D).groups * (D + 255) + 3 * (int64_t)N * D + 256 >= kMaxThreads) return QDELTA_EUNSUPPORTED;
+  // 16 threads a column of the sum over the workgroups
+  if ((dweight || dbias) && 16 * ((int64_t)(W + 1) * D + 63) >= kMaxThreads) return QDELTA_EUNSUPPORTED;
   a.D = D; a.W = W; a.silu = silu != 0; a.ldx = ldx;
   a.x = x; a.w = weight; a.b = bias; a.s0 = initial_state;
   a.dy = dy; a.dsf = d_final_state;

@@ -43,3 +43,14 @@ def test_the_longest_sequence_is_taken(cu):
     for fn, back in ((L.qdelta_scan_fwd, False), (L.qdelta_scan_bwd, True)):
         assert scan(fn, longest, cu, ws=0) == ENOWORKSPACE and scan(fn, 1 << 29, cu) == EUNSUPPORTED
         assert mixer.scan_workspace_bytes(1, longest, 1, 1, 1, 1, cu is not None, back)
+
+
+def test_channels_past_32_bits_or_a_launch_are_refused():
+    """The taps of 2^29 channels are 2^31 values; the weight's gradient of 2^26 is summed by 16 threads for each of 5 x
+    2^26 columns, which would fail after the other gradients have been launched."""
+    step = lambda D, W: mixer.lib().qdelta_conv_step(1, D, W, 1, 1, FAKE, D, FAKE, None, FAKE, FAKE, FAKE, None)     # noqa: E731
+    for D, W in (((1 << 29) + 1, 4), (1 << 29, 4), (1 << 30, 2)):
+        assert conv_fwd(D=D, W=W) == conv_bwd(D=D, W=W) == step(D, W) == EUNSUPPORTED, (D, W)
+        assert mixer.conv_workspace_bytes(1, 1, D, W) == 0
+    assert conv_bwd(D=1 << 26) == conv_bwd(D=1 << 26, dw=None, db=FAKE) == EUNSUPPORTED
+    assert conv_bwd(D=(1 << 29) - 1, ws=0) == ENOWORKSPACE

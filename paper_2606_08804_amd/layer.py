@@ -232,6 +232,9 @@ class QDeltaLayer(torch.nn.Module):
     recurrence on bf16 activations); gates are formed in fp32 (or wider), the
     q and k L2 norms by the library's row-normalisation kernels."""
 
+    # Modules pickled before these options existed have no such attributes.
+    conv_size, out_norm, out_gate = 0, None, False
+
     def __init__(self, d_model, n_heads, head_dk=128, head_dv=128, use_decay=True, qk_norm=True,
                  lambda_bias=-0.8, fixed_lambda=None, conv_size=0, out_norm=None, out_gate=False):
         """fixed_lambda: None for the learned gate lambda_t = sigmoid(W h + b);

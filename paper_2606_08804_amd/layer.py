@@ -334,13 +334,15 @@ class QDeltaLayer(torch.nn.Module):
     def forward(self, h, initial_state=None, cu_seqlens=None, output_final_state=False):
         """initial_state and the final state returned: [N,H,dv,dk], with a
         convolution a pair of that and the convolution's rows [N, conv_size - 1,
-        H (2 dk + dv)]."""
+        H (2 dk + dv)].  Parameters may be wider than the projections' results
+        (fp32 under bf16 autocast): the convolution's and the norm's are then
+        taken in the results' type, as the projections take theirs."""
         B, T, _ = h.shape
         H, dk, dv = self.H, self.dk, self.dv
         qkv = self.w_qkv(h)
         if self.conv_size:
             initial_state, conv_state = (None, None) if initial_state is None else initial_state
-            qkv, conv_state = causal_conv(qkv, self.conv_weight, None, conv_state, cu_seqlens, "silu")
+            qkv, conv_state = causal_conv(qkv, self.conv_weight.to(qkv.dtype), None, conv_state, cu_seqlens, "silu")
         qkv = qkv.view(B, T, H, 2 * dk + dv)
         beta, lam, log_alpha = self._fused_gates(h) if self._can_fuse_gates(h) else self.gates(h)
         gates = (beta.contiguous(), lam.contiguous() if isinstance(lam, torch.Tensor) else lam,
@@ -356,7 +358,8 @@ class QDeltaLayer(torch.nn.Module):
                                           cu_seqlens)
         if self.out_norm:
             gate = self.w_out_gate(h).view(B, T, H, dv) if self.out_gate else None
-            o = row_norm(o, self.norm_weight, self.norm_bias, gate, kind=self.out_norm)
+            bias = None if self.norm_bias is None else self.norm_bias.to(o.dtype)
+            o = row_norm(o, self.norm_weight.to(o.dtype), bias, gate, kind=self.out_norm)
         y = self.w_out(o.reshape(B, T, H * dv))
         if self.conv_size:
             final_state = final_state, conv_state

@@ -206,6 +206,23 @@ def test_norm_several_rows_a_group(D, lanes16, lanes32, kind, gate, dtype):
     assert all(v is None or torch.equal(v, again[name]) for name, v in got.items()), "differs from run to run"
 
 
+def test_norm_of_workgroups_past_one_dimension():
+    """Rows of three bf16 values are one piece: eight lanes, 32 rows a workgroup.  A launch is 2^23 workgroups wide (2^31
+    threads), so that of 32 x 2^23 + 3 rows the last three are in its second row of workgroups.  Equal, bit for bit, to calls
+    on a sixteenth of the rows each."""
+    D = 3
+    lanes, _ = norm_lanes(D, "bf16")
+    rows = 256 // lanes * (1 << 23) + 3
+    g = torch.Generator("cuda").manual_seed(80)
+    x = torch.randint(-300, 300, (rows, D), generator=g, device="cuda", dtype=torch.int16).bfloat16()
+    y, stats = mixer.norm_fwd(x)
+    part = 1 << 24
+    for at in range(0, rows, part):
+        one, st = mixer.norm_fwd(x[at:at + part])
+        assert torch.equal(y[at:at + part], one) and torch.equal(stats[at:at + part], st), at
+    assert not torch.equal(y[-1], y[-2])
+
+
 # ------------------------------------------------------------------------------------------------ scan
 
 def scan64(d, softplus, dy, dsf, pad):

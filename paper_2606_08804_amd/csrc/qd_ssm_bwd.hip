@@ -27,7 +27,10 @@
 //                               read straight from the walks' register order;
 //   wave w, rows 16 w .. of p   G B^T, with G through LDS.
 // A spilled register costs more than its own bytes: its reload waits for every
-// prefetch issued before it.
+// prefetch issued before it.  Within the loop over heads, waves 0 to 3 reload one
+// quad of K a turn in bf16 with N > 64 (none with N <= 64); fp32 with N > 64, where the
+// operands of a product take twice the registers, stores five quads a turn and
+// reloads up to nine.
 //
 // 4 x 4096 tokens, 64 heads of one group, state 64 x 128, bf16: 500 us, 7.8 us a
 // chunk and head.  States and gradients are 1.08 of the 1.57 GB it moves (3.2
@@ -59,9 +62,12 @@ struct BwdLds {
 };
 
 // Sum over the four lane groups (the rows of an accumulator's columns).
+// (The lane number formed here: what __shfl_xor forms of it would be kept over the
+// loops, in scratch memory.)
 __device__ inline float groups_sum(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
+  const int lane = fresh_lane();
+  x += lane_from(x, lane ^ 16);
+  return x + lane_from(x, lane ^ 32);
 }
 
 // Sum over the lanes before this one: the inclusive sum of the lane below, so

@@ -22,8 +22,9 @@
  * groups over all chunks of 64 tokens, or 2^31 heads over all tokens).
  *
  * Precision: sums, statistics and states are fp32.  Exponentials (SiLU, softplus,
- * decays) are good to the last place of fp32; with bf16 activations those of SiLU
- * and of the decays between tokens of a chunk are off by |x| 2^-23. */
+ * the state's decays) are good to the last places of fp32, but for decays between
+ * two tokens of a chunk, off by |x| 2^-24 relative (their argument is rounded),
+ * and, with bf16 activations, for those and SiLU, off by |x| 2^-23. */
 #ifndef QDELTA_MIXER_H
 #define QDELTA_MIXER_H
 

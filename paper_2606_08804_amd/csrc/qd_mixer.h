@@ -71,6 +71,13 @@ template <typename E> __device__ inline float exp_of(float x) {
   if constexpr (sizeof(E) == 2) return fast_exp(x);
   else return expf(x);
 }
+// exp(hi + lo) for lo within hi's last place: exp(hi) alone is off by the lo that
+// its argument has lost, |hi| 2^-24.
+__device__ inline float exp_sum(float hi, float lo) {
+  const float e = expf(hi);
+  return fabsf(hi) < __builtin_inff() ? fmaf(e, lo, e) : e;
+}
+__device__ inline float exp_of64(double x) { return exp_sum((float)x, (float)(x - (double)(float)x)); }
 template <typename E> __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_of<E>(-x)); }
 
 // Sequences of a call: dense (cu == nullptr: N sequences of T tokens) or

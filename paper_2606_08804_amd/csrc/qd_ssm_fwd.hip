@@ -51,10 +51,10 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
     g[2 * C] = (float)(b - (double)(float)b);
     // each from a difference formed in 64 bits
     const double before = __shfl(b, max(lane & ~15, 1) - 1, 64);
-    g[3 * C] = expf((float)b);
-    g[4 * C] = expf((float)(__shfl(b, C - 1, 64) - b));
-    g[5 * C] = expf((float)(lane < 16 ? b : b - before));
-    g[6 * C] = expf((float)(__shfl(b, lane | 15, 64) - b));
+    g[3 * C] = exp_of64(b);
+    g[4 * C] = exp_of64(__shfl(b, C - 1, 64) - b);
+    g[5 * C] = exp_of64(lane < 16 ? b : b - before);
+    g[6 * C] = exp_of64(__shfl(b, lane | 15, 64) - b);
   }
 }
 
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(NTHREADS, 2) QD_TWO_WAVES void k_ssm_walk(ScanArgs 
         const int p = p0 + 16 * w + g4 + j, nn = 16 * nb + col;
         if (p < a.P && nn < a.N) out[(long)p * a.N + nn] = sign * S[nb][j];
       }
-  if (!whole && !keep && dir == dir0 && p0 == 0 && t == 0) a.decay[slot * a.H + h] = (float)run;
+  if (!whole && !keep && dir == dir0 && p0 == 0 && t == 0) a.decay[slot * a.H + h] = exp_of64(run);
 }
 
 // Entries of the segments of each sequence from their own contributions and
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_compose(ScanArgs a, int dir0) 
   for (int j = 0; j < k; ++j) {
     const long slot = base + (dir ? k - 1 - j : j), u = slot * a.H + h;
     a.entry[dir][u * per + i] = S;
-    S = expf(a.decay[u]) * S + a.total[dir][u * per + i];
+    S = a.decay[u] * S + a.total[dir][u * per + i];
   }
   float* out = dir ? a.dS0 : a.Sf;
   if (out) out[at] = S;
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(NTHREADS) void k_ssm_step(ScanArgs a) {
   const int p = (int)(blockIdx.x % per) * 4 * RPW + w * RPW + (lane >> 4), l = lane & 15;
   const int grp = h / (a.H / a.G);
   const float z = a.dt[unit] + (a.bias ? a.bias[h] : 0.f);
-  const float dt = step_size(z, a.softplus), al = expf(dt * a.A[h]);
+  const float dt = step_size(z, a.softplus), da = dt * a.A[h], al = exp_sum(da, fmaf(dt, a.A[h], -da));
   if (p >= a.P) return;
   const float x = tof(((const E*)a.x)[n * a.ldx + (long)h * a.P + p]), dx = dt * x;
   const E* B = (const E*)a.B + n * a.ldb + (long)grp * a.N;

@@ -100,3 +100,40 @@ def test_scan_decays_of_the_state_are_good_to_the_last_places(dtype):
         x[:, 0], B[:, 0], C[:, 1, 0, 0] = 1, 1, 1
         y, _ = mixer.scan_fwd(x, dt.expand(1, 2, H).contiguous(), A, B, C)
         assert not y[:, 0].any() and _off(y[0, 1, :, 0], want) <= 2 * K_EXP       # products in three more roundings
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,H", [(50, 300), (1, 300), (1300, 3)])             # whole sequences; cut into segments
+def test_scan_decays_of_prefix_sums_that_32_bits_round(T, H, dtype):
+    """The state after T tokens that add nothing is exp(sum dt A) to its last places, also where that sum, here from -1 to
+    -80, is no value of fp32 (rounded, it would be off by up to 2^-18): one exponential a chunk and a product a chunk of 21."""
+    g = torch.Generator().manual_seed(T)
+    dt = (0.5 + torch.rand(1, T, H, generator=g)) / T
+    A = -torch.linspace(1, 80, H)
+    want = torch.exp((dt.double() * A.double()).sum(1)[0])
+    z = lambda *s, t=dtype: torch.zeros(s, dtype=t, device="cuda")                # noqa: E731
+    P, N = 4, 4
+    ones = torch.ones(1, H, P, N, device="cuda")
+    args = (z(1, T, H, P), dt.cuda(), A.cuda(), z(1, T, 1, N), z(1, T, 1, N))
+    _, s = mixer.scan_fwd(*args, initial_state=ones)
+    back = mixer.scan_bwd(*args, None, None, ones, z(1, T, H, P), ones)["d_initial_state"]
+    one = ones.clone()
+    if T == 1:
+        mixer.scan_step(*(t[0] if t.dim() > 1 else t for t in args), one)
+    for got in (s, back, one) if T == 1 else (s, back):
+        off = _off(got[0, :, 0, 0], want)
+        assert (got == got[:, :, :1, :1]).all() and off <= 21 * 2.0 ** -23, off
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_scan_time_step_without_end(dtype):
+    """An infinite time step forgets the state: decay 0, not NaN, in prompts and single tokens (x and B are zero where
+    it stands, so that the products with it are NaN there and in what follows; the tokens before are untouched)."""
+    g = torch.Generator().manual_seed(3)
+    r = lambda *s, t=dtype: torch.randn(*s, generator=g).to(t).cuda()             # noqa: E731
+    x, dt, B, C = r(1, 40, 2, 8), r(1, 40, 2, t=torch.float32).abs(), r(1, 40, 1, 8), r(1, 40, 1, 8)
+    A = -torch.ones(2, device="cuda")
+    y, _ = mixer.scan_fwd(x, dt, A, B, C)
+    dt[0, 20, 1] = float("inf")
+    z, s = mixer.scan_fwd(x, dt, A, B, C)
+    assert torch.equal(z[:, :20], y[:, :20]) and torch.equal(z[:, :, 0], y[:, :, 0]) and torch.isfinite(s[0, 0]).all()

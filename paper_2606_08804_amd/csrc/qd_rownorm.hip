@@ -12,7 +12,11 @@
 // formed from there.  16384 rows of 2048 in bf16: forward 26 us (134 MB, 5.1
 // TB/s), backward 44 us (201 MB, 4.5 TB/s); 262144 gated rows of 128: 33 and 60
 // us (201 MB, 6.1 TB/s, and 336 MB, 5.6 TB/s, some of it from the last level
-// cache).  The backward's row groups walk rows with the weight's
+// cache).  Gated rows of 1025 to 2048 and of 4097 to 8192 values in bf16 take all
+// registers in the backward, one wave a SIMD and no row read ahead: on the same
+// tensors again and again, 16384 x 2048 forward 34 us (6.0 TB/s), backward 94 (3.6
+// TB/s), 4096 x 8192 33 and 94.
+// The backward's row groups walk rows with the weight's
 // gradient in registers, sum it over the workgroup in LDS and write one partial
 // row per workgroup; no atomics, so results do not change from run to run.
 #include "qd_mixer.h"
@@ -313,10 +317,13 @@ bool whole(const RowNormArgs& a, int esz) {
 
 }  // namespace
 
-// Workgroups of the backward: enough to fill the chip, few enough that their
-// partial rows (2 D floats each) stay small beside the tensors (forward and
-// backward with 256, 512 and 1024: 16384 x 2048 in bf16 81, 78, 88 us; 262144
-// gated rows of 128 with 1024 and 2048: 93 and 99 us).
+// Workgroups of the backward: enough to fill the chip, few enough that the partial
+// rows (2 D floats each) of large calls stay small beside their tensors (forward
+// and backward repeated on the same tensors with 256, 512 and 1024: 16384 x 2048 in
+// bf16 78, 71, 82 us; 262144 gated rows of 128 with 512, 1024 and 2048: 106, 95, 99).
+// Counted by rows, not by the rows a workgroup takes: calls of fewer rows than these
+// workgroups take have some without any, which write zeros (777 x 1003 in fp32: 582 of
+// 777; backward and column sum 15 us of a call's 30).
 int norm_bwd_blocks(long rows, int D) {
   long n = (1L << 20) / D;
   n = n < 256 ? 256 : n > 1024 ? 1024 : n;

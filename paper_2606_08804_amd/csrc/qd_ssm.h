@@ -10,7 +10,7 @@
 // x = hi + mid + lo, which is exact.  Two of them are off by up to 2^-16: results
 // that are rounded to bf16 afterwards then differ from those of fp32 products in
 // one of 500 (dB, dC) to 1500 values (y), and cost a tenth less (4 x 4096 tokens, 64
-// heads, training 1012 us instead of 1103; a prompt of 65536, 16 heads, 594 and 675).
+// heads, training 1012 us instead of 1098; a prompt of 65536, 16 heads, 594 and 664).
 #pragma once
 
 #include "qd_mixer.h"
@@ -296,7 +296,8 @@ struct Stage {
   }
   // Nothing is loaded where rows are not whole pieces: `put` then reads them, a
   // piece from any element on (4 x 1024 tokens, 32 heads, state 64 x 100, training
-  // in bf16: 279 us; value by value 533, whole pieces of 64 x 128 214).
+  // in bf16: 275 us, whole pieces of 64 x 128 196; value by value it took 533 where
+  // these were 279 and 214).
   __device__ inline void load(const E* src, long ld, int rows, bool vec, uint32_t off) {
     const __amdgpu_buffer_rsrc_t b = buffer(uniform_ptr(src), vec ? (uint32_t)(rows * ld) * (uint32_t)sizeof(E) : 0u);
 #pragma unroll

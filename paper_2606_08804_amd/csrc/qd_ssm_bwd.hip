@@ -32,9 +32,9 @@
 // operands of a product take twice the registers, stores five quads a turn and
 // reloads up to nine.
 //
-// 4 x 4096 tokens, 64 heads of one group, state 64 x 128, bf16: 500 us, 7.8 us a
-// chunk and head.  States and gradients are 1.08 of the 1.57 GB it moves (3.2
-// TB/s); vector instructions take 46% of the cycles and matrix products 19%,
+// 4 x 4096 tokens, 64 heads of one group, state 64 x 128, bf16: 541 us, 8.5 us a
+// chunk and head.  States and gradients are 1.08 of the 1.61 GB it moves (3.0
+// TB/s); vector instructions take 48% of the cycles and matrix products 21%,
 // on two waves a SIMD, which the registers (256 each) and LDS allow.
 #include "qd_ssm.h"
 
@@ -78,8 +78,8 @@ __device__ inline float before_lane(float x, int lane) {
 }
 
 // WHOLE: all rows of x, dy, B and C are whole aligned pieces; without the other
-// way of reading them in the loops a training step of the size above takes 1013
-// us instead of 1027.
+// way of reading them in the loops a training step of the size above takes 1058
+// us instead of 1062, repeated on the same tensors.
 template <typename E, int NP, bool WHOLE>
 __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_bwd(ScanArgs a, long items) {
   typedef BwdLds<E, NP> L;
@@ -642,7 +642,7 @@ hipError_t chunks(const ScanArgs& a, hipStream_t st) {
 
 // Workgroups that share the heads of a chunk: as many as give every CU one, and
 // no more than the largest share needs (1 x 4096 tokens of 64 heads, training
-// step with 1, 2, 4, 8 and 16: 669, 470, 378, 397, 433 us; the rule takes 4).
+// step with 1, 2, 4, 8 and 16: 718, 494, 399, 413, 450 us; the rule takes 4).
 int scan_splits(const Seqs& q, int H, int G) {
   const long units = q.slots(C) * G, cus = device_cu_count(), heads = H / G;
   if (units <= 0) return 1;

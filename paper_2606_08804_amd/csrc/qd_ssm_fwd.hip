@@ -27,7 +27,7 @@ namespace {
 
 // Gates of a chunk slot's 16 heads a workgroup: the raw steps are read along
 // the heads, transposed in LDS, then a token is a lane.
-// 16384 tokens of 64 heads: 12 us, 29 MB written.
+// 16384 tokens of 64 heads: 13 us, 29 MB written.
 __global__ __launch_bounds__(NTHREADS) void k_ssm_gates(ScanArgs a) {
   __shared__ float raw[16][C + 1];
   const int hb = (a.H + 15) / 16, h0 = (int)(blockIdx.x % hb) * 16, t = threadIdx.x, lane = t & 63, w = wave_id(t);
@@ -90,12 +90,12 @@ struct OutLds {
 // barriers, after the operands are in LDS and at the end.  fp32 with N > 64
 // has room for one chunk in LDS only: there the two halves take turns.
 //
-// 4 x 4096 tokens, 64 heads, state 64 x 128, bf16: 225 us, one walk a CU, 3.5 us
-// a chunk (270 MB, 1.2 TB/s; 65536 tokens, 16 heads, 128 x 128: 444 us).  The
+// 4 x 4096 tokens, 64 heads, state 64 x 128, bf16: 261 us, one walk a CU, 4.1 us
+// a chunk (270 MB, 1.0 TB/s; 65536 tokens, 16 heads, 128 x 128: 513 us).  The
 // chain of a chunk bounds it: two barriers, vector instructions 38% of the
 // cycles (planes of the state and of the weighted x), matrix products 21%.
 // Producers and consumers on the same SIMDs fill each other's waits; all eight
-// waves doing both took 350 us.
+// waves doing both took 350 us where this form took 236 (two planes a product).
 template <typename E, int NP>
 __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanArgs a, long items) {
   typedef OutLds<E, NP> L;
@@ -393,7 +393,7 @@ __global__ __launch_bounds__(2 * NTHREADS, 1) QD_TWO_WAVES void k_ssm_out(ScanAr
 // sequence.  Accumulators [p][n]: f4 S[nb] holds rows p = 16 w + g4 + j of
 // column n = 16 nb + col, which is also the order in `states` and `grads`: a
 // wave's stores are whole and the backward's loads are operands as they come.
-// Both directions in one launch, 4 x 4096 tokens, 64 heads, state 64 x 128: 283
+// Both directions in one launch, 4 x 4096 tokens, 64 heads, state 64 x 128: 280
 // us for 1.08 GB written and 0.37 read (5.1 TB/s): bound by HBM.
 template <typename E, int NP>
 struct WalkLds {
@@ -632,12 +632,12 @@ hipError_t launch_scan_compose(const ScanArgs& a, int dirs, hipStream_t st) {
 
 // Walks are serial over their chunks, so a call of few heads is cut into
 // segments until two of them run on every CU (16 heads of 128 x 128, bf16
-// prompts, segments for one, two and four a CU: 65536 tokens 604, 560, 577 us,
-// 16384 tokens 164, 159, 181; uncut 3190 and 745).  A segment costs a second
+// prompts, segments for one, two and four a CU: 65536 tokens 685, 638, 653 us,
+// 16384 tokens 181, 176, 197; uncut 3754 and 890).  A segment costs a second
 // walk without outputs and its state, so it has eight chunks at least in bf16
-// (4096 tokens, four and eight chunks: 71 and 64 us) and two in fp32, where a
+// (4096 tokens, four and eight chunks: 77 and 70 us) and two in fp32, where a
 // chunk takes longer (3001 packed tokens of 8 heads of 64 x 64, forward and
-// backward, two, four and eight: 136, 157 and 194 us).
+// backward, two, four and eight: 116, 139 and 168 us).
 int scan_segment(const Seqs& q, int H, int P, int dirs, bool f32) {
   const long tokens = q.cu ? q.T : (long)q.N * q.T, want = 2L * device_cu_count();
   const long units = (long)q.N * H * p_tiles(P) * dirs;

@@ -323,3 +323,43 @@ def test_scan_several_heads_a_workgroup(lens, packed, H, G, P, N, seg, splits, d
     again = back()
     assert all(torch.equal(got[k], again[k]) for k in got), "differs from run to run"
     assert math.prod(got["dB"].shape) == T * lead[0] * G * N
+
+
+def test_offsets_past_32_bits():
+    """2.2e9 values of 8192 a token: the last tokens are those of calls on them alone, with the rows before them as the
+    convolution's state and a time step that wipes the scan's.  Bit for bit where a value does not depend on where its tile or
+    segment begins; the scan's by 2^-20 of the largest (states are put together in another order)."""
+    g = torch.Generator("cuda").manual_seed(81)
+    big = lambda *s: torch.randn(s, generator=g, device="cuda", dtype=torch.bfloat16)          # noqa: E731
+    D, n, T = 8192, 1000, (1 << 18) + 4100
+    x, w, b = big(1, T, D), big(D, 4), big(D)
+    last = lambda t: t[:, -n:].contiguous()                                      # noqa: E731
+    assert x[:, :-n].numel() > 1 << 31
+    y, state = mixer.conv_fwd(x, w, b, activation="silu")
+    dx = mixer.conv_bwd(x, w, b, None, x, activation="silu")["dx"]
+    before = x[:, -n - 3:-n].contiguous()
+    y1, state1 = mixer.conv_fwd(last(x), w, b, before, activation="silu")
+    dx1 = mixer.conv_bwd(last(x), w, b, before, last(x), activation="silu")["dx"]
+    assert torch.equal(last(y), y1) and torch.equal(state, state1) and torch.equal(last(dx), dx1)
+
+    y, stats = mixer.norm_fwd(x, b)
+    dx = mixer.norm_bwd(x, b, None, None, stats, x)["dx"]
+    y1, stats1 = mixer.norm_fwd(last(x), b)
+    assert torch.equal(last(y), y1) and torch.equal(last(stats), stats1)
+    assert torch.equal(last(dx), mixer.norm_bwd(last(x), b, None, None, stats1, last(x))["dx"])
+
+    H, N, at = 64, 16, T // 64 * 64 - 1024
+    x = x.unflatten(2, (H, D // H))
+    B, C, A = big(1, T, 1, N), big(1, T, 1, N), -torch.ones(H, device="cuda")
+    dt = 0.1 * torch.rand(1, T, H, generator=g, device="cuda")
+    dt[:, at] = 1000
+    last = lambda t: t[:, at:].contiguous()                                      # noqa: E731
+    far = lambda a, e: float((a.double() - e.double()).abs().max() / e.double().abs().max())   # noqa: E731
+    y, state = mixer.scan_fwd(x, dt, A, B, C)
+    y1, state1 = mixer.scan_fwd(last(x), last(dt), A, last(B), last(C))
+    assert far(state, state1) <= 2.0 ** -20 and far(last(y), y1) <= 2.0 ** -7    # y: a bf16 rounding to the other side
+    got = mixer.scan_bwd(x, dt, A, B, C, None, None, None, x)
+    want = mixer.scan_bwd(last(x), last(dt), A, last(B), last(C), None, None, None, last(x))
+    for k in ("dx", "dB", "dC"):
+        assert far(last(got[k]), want[k]) <= 2.0 ** -7, k
+    assert far(last(got["ddt"]), want["ddt"]) <= 2.0 ** -20

@@ -96,11 +96,14 @@ int qdelta_norm_bwd(int64_t rows, int32_t D, int32_t dtype, int32_t rms, const v
  *   dt [tokens, H], A [H], D, dt_bias [H] or NULL           float32 (dt A <= 0 expected)
  *   initial_state, final_state [N, H, P, Ns] or NULL        float32 (NULL: zero, not wanted)
  *   y [tokens, H, P]   (dtype)
- * P is at most 256, Ns at most 128 and G divides H (else QDELTA_EUNSUPPORTED,
- * QDELTA_EINVAL).  Prompts go by chunks of 64 tokens on the matrix cores: bf16
- * products of values that are fp32 take them as sums of bf16 values, so that
- * states and their gradients keep fp32's precision.  Packing does not change a
- * sequence's chunks.  Workspace of qdelta_scan_workspace_bytes. */
+ * dt A > 0 is taken as well; growth past fp32 (e^88) within 64 tokens leaves
+ * infinities or NaN.  P is at most 256, Ns at most 128 and G divides H (else
+ * QDELTA_EUNSUPPORTED, QDELTA_EINVAL).  Prompts go by chunks of 64 tokens on the
+ * matrix cores: bf16 products of values that are fp32 take them as sums of three
+ * bf16 values, which are exact, so that every result keeps fp32's precision until
+ * it is rounded to its type.  An infinity in x, B, C or a state may come out as a
+ * NaN in what it enters.  Packing does not change a sequence's chunks.  Workspace
+ * of qdelta_scan_workspace_bytes. */
 size_t qdelta_scan_workspace_bytes(int32_t N, int32_t T, int32_t packed, int32_t H, int32_t G, int32_t P, int32_t Ns,
                                    int32_t is_bwd);
 int qdelta_scan_fwd(int32_t N, int32_t T, const int32_t* cu_seqlens, int32_t H, int32_t G, int32_t P, int32_t Ns,

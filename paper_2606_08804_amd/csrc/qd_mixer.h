@@ -72,10 +72,10 @@ template <typename E> __device__ inline float exp_of(float x) {
   else return expf(x);
 }
 // exp(hi + lo) for lo within hi's last place: exp(hi) alone is off by the lo that
-// its argument has lost, |hi| 2^-24.
+// its argument has lost, |hi| 2^-24.  (An infinite hi or e leaves no such product.)
 __device__ inline float exp_sum(float hi, float lo) {
-  const float e = expf(hi);
-  return fabsf(hi) < __builtin_inff() ? fmaf(e, lo, e) : e;
+  const float e = expf(hi), f = fmaf(e, lo, e);
+  return f == f ? f : e;
 }
 __device__ inline float exp_of64(double x) { return exp_sum((float)x, (float)(x - (double)(float)x)); }
 template <typename E> __device__ inline float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + exp_of<E>(-x)); }

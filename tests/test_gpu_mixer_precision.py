@@ -137,3 +137,25 @@ def test_scan_time_step_without_end(dtype):
     dt[0, 20, 1] = float("inf")
     z, s = mixer.scan_fwd(x, dt, A, B, C)
     assert torch.equal(z[:, :20], y[:, :20]) and torch.equal(z[:, :, 0], y[:, :, 0]) and torch.isfinite(s[0, 0]).all()
+
+
+@pytest.mark.parametrize("T", [1, 50, 1300])
+def test_scan_growth_past_fp32_is_not_finite(T):
+    """dt A > 0 is not expected, and not refused.  A state that grows is exp(sum dt A); past fp32 it becomes an infinity of
+    its sign, or, where that happens within a chunk whose weights overflow too (they meet the zeros of x), a NaN."""
+    H, P, N = 2, 4, 4
+    z = lambda *s: torch.zeros(s, device="cuda")                                 # noqa: E731
+    dt, A = torch.full((1, T, H), 1.0 / T).cuda(), torch.tensor([80.0, 100.0]).cuda()
+    s0 = torch.tensor([1.0, -1.0], device="cuda").repeat(2)[:, None].expand(1, H, P, N).contiguous()
+    args = (z(1, T, H, P), dt, A, z(1, T, 1, N), z(1, T, 1, N))
+    _, s = mixer.scan_fwd(*args, initial_state=s0)
+    got = [s]
+    if T == 1:
+        got.append(s0.clone())
+        mixer.scan_step(*(t[0] if t.dim() > 1 else t for t in args), got[1])
+    want = torch.exp((dt.double().cpu() * A.double().cpu()).sum(1))[0, 0] * s0[0, 0].double().cpu()
+    for s in got:
+        assert _off(s[0, 0], want) <= 21 * 2.0 ** -23
+        assert not torch.isfinite(s[0, 1]).any()
+        if T != 50:
+            assert torch.equal(s[0, 1], s0[0, 1] * float("inf"))
